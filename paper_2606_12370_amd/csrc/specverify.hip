@@ -14,6 +14,7 @@
 
 #include "specverify.h"
 #include "sv_device.h"
+#include "sv_host.h"
 #include "gumbel_kernel.h"
 #include "kl_kernel.h"
 #include "tv_kernel.h"
@@ -26,6 +27,10 @@ namespace {
 
 using sv::BF16;
 using sv::F32;
+using sv::align_up;
+using sv::aligned16;
+using sv::esize_of;
+using sv::extent_ok;
 
 // Chunk geometry: a chunk is NT tiles of one 16-byte vector per thread,
 // 16384 elements for both dtypes, read S tiles per step.
@@ -88,8 +93,6 @@ template <> struct GradElem<sv::BF16> { using type = sv::BF16H; };
 
 int epv_of(spec_dtype dt) { return dt == SPEC_BF16 ? BF16::EPV : F32::EPV; }
 int nt_of(spec_dtype dt) { return dt == SPEC_BF16 ? kNtBf16 : kNtF32; }
-size_t esize_of(spec_dtype dt) { return dt == SPEC_BF16 ? 2 : 4; }
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Geometry {
   int ntiles = 0;  // tiles per row
@@ -233,25 +236,11 @@ DiagLayout diag_layout(int B, int K, int V, spec_dtype dt) {
   return L;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 // Both strides keep 16-byte vectors aligned (the products are taken modulo
 // 2^64, which leaves them unchanged modulo 16).
 bool rows_vec_aligned(const void* base, int64_t s0, int64_t s1, size_t esize) {
   return aligned16(base) && (static_cast<uint64_t>(s0) * esize) % 16 == 0 &&
          (static_cast<uint64_t>(s1) * esize) % 16 == 0;
-}
-
-// The last byte a tensor of n0 x n1 rows of V elements (strides s0, s1 in
-// elements, both >= 0) occupies from base lies within the address space: the
-// kernels' 64-bit row offsets then never overflow.
-bool extent_ok(const void* base, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int V, size_t esize) {
-  int64_t a, b, last, bytes;
-  if (__builtin_mul_overflow(n0 - 1, s0, &a) || __builtin_mul_overflow(n1 - 1, s1, &b) ||
-      __builtin_add_overflow(a, b, &last) || __builtin_add_overflow(last, static_cast<int64_t>(V), &last) ||
-      __builtin_mul_overflow(last, static_cast<int64_t>(esize), &bytes))
-    return false;
-  uintptr_t end;
-  return !__builtin_add_overflow(reinterpret_cast<uintptr_t>(base), static_cast<uintptr_t>(bytes), &end);
 }
 
 // Statistics per sub-chunk of every row, one wave per sub-chunk and four

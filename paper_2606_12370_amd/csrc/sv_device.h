@@ -430,18 +430,6 @@ __device__ __forceinline__ RowNorm make_norm(float M, double D) {
 }
 __device__ __forceinline__ bool norm_ok(const RowNorm& n) { return n.D > 0.0 && n.D < INFINITY && n.M < INFINITY; }
 
-// One wave per row: combine every row's chunk statistics (4 rows per
-// 256-thread workgroup).
-__global__ __launch_bounds__(kThreads) void row_norm_kernel(const RowStat* __restrict__ stats, int rows, int C,
-                                                            RowNorm* __restrict__ out) {
-  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (r >= rows) return;
-  float M;
-  double D;
-  combine_row(stats + static_cast<int64_t>(r) * C, C, &M, &D);
-  if ((threadIdx.x & 63) == 0) out[r] = make_norm(M, D);
-}
-
 // Probability of one element given its row's (M, 1/D): 2^(z s - M) / D.
 __device__ __forceinline__ float prob(float z, float s, float M, float invD) {
   return __builtin_amdgcn_exp2f(fmaf(z, s, -M)) * invD;

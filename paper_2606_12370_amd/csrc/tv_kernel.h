@@ -5,7 +5,7 @@
 //
 //   1 row_stats   (sv_device.h) per-chunk statistics of every target and
 //                 draft row of the N positions x K steps.
-//   2 row_norm    (sv_device.h) each row's normaliser.
+//   2 row_norm    each row's normaliser.
 //   3 tv_pair     per (position n, step k, chunk): alpha partial sum min(p, q),
 //                 S partial sum 1[q <= p] q and its complement 1 - S summed
 //                 directly as sum 1[q > p] q (where one token holds nearly
@@ -28,6 +28,18 @@
 #include "sv_device.h"
 
 namespace sv {
+
+// One wave per row: combine every row's chunk statistics (4 rows per
+// 256-thread workgroup).
+__global__ __launch_bounds__(kThreads) void row_norm_kernel(const RowStat* __restrict__ stats, int rows, int C,
+                                                            RowNorm* __restrict__ out) {
+  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  float M;
+  double D;
+  combine_row(stats + static_cast<int64_t>(r) * C, C, &M, &D);
+  if ((threadIdx.x & 63) == 0) out[r] = make_norm(M, D);
+}
 
 struct TvPair {
   double alpha;
