@@ -1,0 +1,170 @@
+/*
+ * specverify_rollout.h — the calls of libspecverify.so for engines that keep
+ * or exchange less than whole rows of logits: verification from probabilities
+ * and random numbers of their own, the record of a target row as its largest
+ * logits, and the distillation of a draft from such records.
+ *
+ * The conventions are those of specverify.h (device pointers and element
+ * strides, work enqueued on `stream` only, no allocation, a caller-owned
+ * workspace that carries nothing between calls, host-checkable errors returned
+ * before any work).  Calls that share a workspace must not run concurrently;
+ * that includes replays of captured graphs.  Outputs must not overlap inputs,
+ * the workspace or each other.  The current device must be the one that holds
+ * the tensors.  No launch waits on another workgroup.
+ */
+#ifndef SPECVERIFY_ROLLOUT_H
+#define SPECVERIFY_ROLLOUT_H
+
+#include "specverify.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define SPEC_MAX_LIST 256 /* longest list of top logits */
+
+/* Bytes of workspace spec_top_logits needs (0 on invalid sizes). */
+size_t spec_top_logits_workspace_size(int N, int K, int V, int M, spec_dtype dtype);
+
+/*
+ * spec_top_logits — the M largest logits of every row and the row's log
+ * partition function.
+ *
+ * For row (n, k) of logits [N, K, V], T = temperature[n] (or temperature_scalar):
+ *   values[n, k, 0..M-1]  the largest logits, largest first, as they are (not
+ *                         divided by T); equal logits in the order of their
+ *                         indices (0 and -0 are equal)
+ *   ids[n, k, 0..M-1]     their indices
+ *   logz[n, k]            log sum_v exp(logits[n, k, v] / T)
+ * Logits of -inf (masked tokens) are never listed: a row with fewer than M
+ * others ends in entries with id -1 and value -inf, and a row of nothing else
+ * is such a list throughout, with logz = -inf.
+ *
+ * logits         [N, K, V] element strides (stride_n, stride_k), dtype
+ * temperature    [N] float32 device array, or NULL: temperature_scalar (finite, > 0)
+ * ids            [N, K, M] int32 out, contiguous
+ * values         [N, K, M] float32 out, contiguous
+ * logz           [N, K] float32 out (may be NULL)
+ * workspace      device memory of at least spec_top_logits_workspace_size bytes
+ * Row data errors (NaN or +inf logits, a per-row temperature that is not
+ * finite and > 0) give ids -1, values NaN and logz NaN.
+ * Limits: 1 <= M <= SPEC_MAX_LIST (SPEC_EUNSUPPORTED beyond), 1 <= V <=
+ * SPEC_MAX_V, 1 <= N, 1 <= K, N*K < 2^31.
+ */
+spec_status spec_top_logits(const void* logits, int64_t stride_n, int64_t stride_k, spec_dtype dtype,
+                            int N, int K, int V, int M,
+                            const float* temperature, float temperature_scalar,
+                            int32_t* ids, float* values, float* logz,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+typedef enum SPEC_ENUM_INT {
+  SPEC_DISTILL_FORWARD = 0, /* sum_j p_j log(p_j / q_j) (+ the same of the mass outside the list) */
+  SPEC_DISTILL_CE = 1       /* -sum_j p_j log q_j (likewise)                                      */
+} spec_distill_kind;
+
+/* Bytes of workspace spec_distill_loss_fwd_bwd needs (0 on invalid sizes). */
+size_t spec_distill_workspace_size(int N, int K, int V, int M, spec_dtype dtype);
+
+/*
+ * spec_distill_loss_fwd_bwd — distillation of the draft from a teacher's top
+ * logits, and its gradient w.r.t. the draft logits: the forward-KL / CE
+ * objectives of spec_kl_loss_fwd_bwd for a teacher row known by its list only.
+ *
+ * For position n and draft step k, q = softmax(draft[n, k] / T) and the list's
+ * entries j with id_j >= 0:
+ *   p_j = exp(t_j / T) / sum_i exp(t_i / T)       without teacher_logz
+ *   p_j = exp(t_j / T - teacher_logz[n, k])       with it (log Z at the same T);
+ *         the mass outside the list, r = 1 - sum_j p_j, is then one more
+ *         outcome, whose draft probability q_out is the sum of q over the
+ *         tokens not listed.  (r <= 2^-18, which a float32 log Z does not
+ *         resolve, counts as 0; without teacher_logz r = 0.)
+ *   forward KL  L_{n,k} = sum_j p_j log(p_j / q_id_j) + r log(r / q_out)
+ *   CE          L_{n,k} = -sum_j p_j log q_id_j - r log q_out
+ *   grad[n, k, v] = scale * (1/K) * (1/T) * ((W + r) q_v - sum_{j: id_j = v} p_j
+ *                   - (v not listed) r q_v / q_out),  W = sum_j p_j
+ *   loss = scale * sum_n (1/K) sum_k L_{n,k}
+ * An id listed twice counts with both entries' probabilities.  Terms with
+ * p_j = 0 are 0.  A position without entries (all ids < 0; without
+ * teacher_logz also all values -inf) has L = 0 and a gradient of zeros.
+ *
+ * draft_logits    [N, K, V] element strides (d_stride_n, d_stride_k), dtype
+ * teacher_ids     [N, K, M] int32, teacher_values [N, K, M] float32, both with
+ *                 element strides (l_stride_n, l_stride_k), the lists contiguous
+ * teacher_logz    [N, K] float32, strides (z_stride_n, z_stride_k), or NULL
+ * temperature     finite and > 0
+ * loss            [1] float32 out
+ * per_step        [N, K] float32 out: L_{n,k} (may be NULL)
+ * grad_draft      [N, K, V] out, contiguous, of grad_dtype; NULL = forward only
+ * grad_dtype      SPEC_F32, or the draft logits' dtype (rounded once, to nearest)
+ * workspace       device memory of at least spec_distill_workspace_size bytes
+ * Data errors (an id >= V, a NaN among teacher_values or in teacher_logz, a
+ * value of +inf, an infinite teacher_logz of a non-empty list, NaN or +inf
+ * draft logits or a row of -inf alone under a non-empty list) make that
+ * position's loss and gradient NaN; a draft logit of -inf under p_j > 0 makes
+ * its forward KL or CE +inf.  The draft logits of an empty list are not read.
+ * Limits: 1 <= M <= SPEC_MAX_LIST (SPEC_EUNSUPPORTED beyond), 1 <= K <=
+ * SPEC_MAX_K, 1 <= V <= SPEC_MAX_V, 1 <= N, N*K < 2^31.
+ */
+spec_status spec_distill_loss_fwd_bwd(const void* draft_logits, int64_t d_stride_n, int64_t d_stride_k,
+                                      spec_dtype dtype, int N, int K, int V,
+                                      const int32_t* teacher_ids, const float* teacher_values,
+                                      int64_t l_stride_n, int64_t l_stride_k, int M,
+                                      const float* teacher_logz, int64_t z_stride_n, int64_t z_stride_k,
+                                      float temperature, spec_distill_kind kind, float scale,
+                                      float* loss, float* per_step, void* grad_draft, spec_dtype grad_dtype,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace spec_verify_probs needs (0 on invalid sizes). */
+size_t spec_verify_probs_workspace_size(int B, int K, int V, spec_dtype dtype);
+
+/*
+ * spec_verify_probs — chain rejection-sampling verification (spec_verify) from
+ * given probabilities and given uniforms, for engines that truncate, renormalise
+ * or share distributions themselves, or bring their own random numbers.
+ *
+ * For row b, len = draft_lens[b] (or K):
+ *   step i < len accepts x_i = draft_ids[b, i] iff u_i * q_i(x_i) < p_i(x_i),
+ *       u_i = accept_uniforms[b, i] (the comparison is exact)
+ *   n = first rejected step (len if none); accept_len[b] = n
+ *   emitted[b, 0..n-1] = x_0..x_{n-1}
+ *   emitted[b, n] = smallest v with C(v) > u' * Z, u' = sample_uniforms[b], C the
+ *       cumulative sum (vocabulary order, float64) of r = max(0, p_n - q_n) if
+ *       n < len, else of r = p_len; Z = sum r.  If Z is 0 after a rejection the
+ *       token is drawn from p_n.  (u' = 1: the last token with mass.)
+ *   emitted[b, n+1..K] = -1
+ *   overlap[b, i] = sum_v min(p_i(v), q_i(v)) for i < len, 0 beyond
+ * The probabilities are taken as given: a row need not sum to 1.
+ * Without draft_probs the drafts are one-hot (a draft without probabilities: a
+ * lookup, a greedy head): q_i(x_i) = 1 and 0 elsewhere, r(x_n) = 0.
+ *
+ * target_probs     [B, K+1, V] element strides (t_stride_b, t_stride_k), dtype
+ * draft_probs      [B, K, V] element strides (d_stride_b, d_stride_k), dtype, or NULL
+ * draft_ids        [B, K] int32, contiguous (NULL if K = 0); entries at and
+ *                  beyond a row's length are not read, nor are accept_uniforms'
+ * accept_uniforms  [B, K] float32 in [0, 1], contiguous (NULL if K = 0)
+ * sample_uniforms  [B] float32 in [0, 1]
+ * draft_lens       [B] int32 in [0, K], or NULL: K for every row
+ * accept_len       [B] int32 out; emitted_ids [B, K+1] int32 out, contiguous
+ * overlap          [B, K] float32 out, or NULL (then only the emitting step's
+ *                  rows are read)
+ * workspace        device memory of at least spec_verify_probs_workspace_size bytes
+ * Row data errors (an id outside [0, V), a length outside [0, K], a uniform
+ * outside [0, 1] or NaN, a probability p_i(x_i), q_i(x_i), i < len, or one of
+ * the emitting step's rows that is negative, infinite or NaN, no mass in p_n)
+ * give accept_len = -1, emitted = -1 and NaN overlaps.  A bad probability
+ * elsewhere in another step's rows makes that step's overlap NaN.
+ * Limits: 0 <= K <= SPEC_MAX_K, 1 <= V <= SPEC_MAX_V, 1 <= B.
+ */
+spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int64_t t_stride_k,
+                              const void* draft_probs, int64_t d_stride_b, int64_t d_stride_k,
+                              spec_dtype dtype, int B, int K, int V,
+                              const int32_t* draft_ids, const float* accept_uniforms,
+                              const float* sample_uniforms, const int32_t* draft_lens,
+                              int32_t* accept_len, int32_t* emitted_ids, float* overlap,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* SPECVERIFY_ROLLOUT_H */

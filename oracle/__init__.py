@@ -22,6 +22,8 @@ gumbel   Gumbel-max verification (App. G.2, Alg. rs_gumbel) and the
          Gumbel-max draft sampler.
 kl       CE, forward-KL and reverse-KL losses and gradients (Sec. 4.1 and its
          footnote, Table grad_comparison, App. B, App. C).
+rollout  Top logits, distillation from them, verification from given
+         probabilities and uniforms.
 
 Every function is pinned by the ``-m "not gpu"`` tests against something
 other than itself (numpy's own Philox, scipy routines, closed forms,

@@ -1,0 +1,194 @@
+"""Top logits, distillation from them, and verification from given
+probabilities, in float64.
+
+TEST INFRASTRUCTURE ONLY (see the package docstring).  Definitions:
+
+top logits    per row the M largest finite logits, largest first, ties to the
+              lowest index, and log sum exp(z / T).
+distillation  p_j = exp(t_j / T - lse) over the list's entries, lse their own
+              log sum or a given log Z (then r = 1 - sum p is the mass outside,
+              0 where at most 2^-18); L = sum p (log p - log q) + r (log r - log
+              q_out), without log p and log r for cross entropy;
+              dL/dz_v = (1/T)((W + r) q_v - sum_{id_j = v} p_j - [v unlisted] r q_v / q_out).
+verification  accept u q < p; first rejection n; token = first v with C(v) > u' Z.
+"""
+
+import numpy as np
+
+TAIL_MIN = 2.0 ** -18
+
+
+def top_ref(logits, M, T):
+    """logits [R, V] float64, T scalar or [R].  Returns ids, values [R, M], logz [R]."""
+    z = np.asarray(logits, dtype=np.float64)
+    R, V = z.shape
+    T = np.broadcast_to(np.asarray(T, dtype=np.float64), (R,))
+    ids = np.full((R, M), -1, np.int32)
+    values = np.full((R, M), -np.inf)
+    logz = np.full(R, -np.inf)
+    spread = np.zeros(R)  # mean of (max - z) / T under the row's softmax: how far rounding reaches
+    for r in range(R):
+        if np.any(np.isnan(z[r])) or np.any(np.isposinf(z[r])) or not (T[r] > 0 and np.isfinite(T[r])):
+            values[r], logz[r] = np.nan, np.nan
+            continue
+        order = np.argsort(-z[r], kind="stable")  # stable: ties in index order (0 and -0 are equal)
+        order = order[z[r][order] > -np.inf][:M]
+        ids[r, :len(order)] = order
+        values[r, :len(order)] = z[r][order]
+        if len(order):
+            d = (z[r] - z[r].max()) / T[r]
+            e = np.exp(d)
+            logz[r] = z[r].max() / T[r] + np.log(e.sum())
+            spread[r] = -(np.where(e > 0, d, 0.0) * e).sum() / e.sum()
+    return dict(ids=ids, values=values, logz=logz, spread=spread)
+
+
+def distill_ref(draft_logits, ids, values, logz, T, kind, scale=1.0):
+    """draft_logits [N, K, V], ids / values [N, K, M], logz [N, K] or None,
+    kind "forward" or "ce".  Returns per_step, loss, grad, and grad_err /
+    step_err: the error per unit of 2^-24 that float32 exponentials and sums of
+    32 may leave in them, and grad_unit, the gradient of the smallest exponential
+    (see the comments)."""
+    z = np.asarray(draft_logits, dtype=np.float64)
+    N, K, V = z.shape
+    per = np.zeros((N, K))
+    step_err = np.zeros((N, K))
+    grad = np.zeros((N, K, V))
+    grad_err = np.zeros((N, K, V))
+    grad_unit = np.zeros((N, K))
+    f = scale / (K * T)
+    for n in range(N):
+        for k in range(K):
+            i, t = np.asarray(ids[n, k]), np.asarray(values[n, k], dtype=np.float64)
+            lz = None if logz is None else float(logz[n, k])
+            used = i >= 0
+            if np.any(np.isnan(t)) or np.any(i >= V) or np.any(np.isposinf(t[used])) or (lz is not None and np.isnan(lz)):
+                per[n, k], grad[n, k] = np.nan, np.nan
+                continue
+            i, t = i[used], t[used]
+            if not len(i) or (lz is None and not np.any(t > -np.inf)):
+                continue
+            if lz is not None and not np.isfinite(lz):
+                per[n, k], grad[n, k] = np.nan, np.nan
+                continue
+            lse = lz if lz is not None else t.max() / T + np.log(np.exp((t - t.max()) / T).sum())
+            lp = t / T - lse
+            p = np.exp(lp)
+            W = p.sum()
+            r = 0.0
+            if lz is not None and 1.0 - W > TAIL_MIN:
+                r = 1.0 - W
+            row = z[n, k]
+            if np.any(np.isnan(row)) or np.any(np.isposinf(row)) or not np.any(row > -np.inf):
+                per[n, k], grad[n, k] = np.nan, np.nan
+                continue
+            d = (row - row.max()) / T
+            e = np.exp(d)
+            dz = np.where(e > 0, -d, 0.0)
+            lq = d - np.log(e.sum())
+            q = np.exp(lq)
+            out = np.ones(V, bool)
+            out[i] = False
+            live = p > 0
+            L = -(p[live] * lq[i][live]).sum()
+            if kind == "forward":
+                L += (p[live] * lp[live]).sum()
+            # each exponential is off by the roundings of the difference and of
+            # the exponent (2 |d| 2^-24 / T) and its own (2), a float32 sum of
+            # 32 by 31 more
+            sp = 33 + 2 * (dz * q).sum()
+            serr = W * sp
+            g = (W + r) * q
+            gerr = g * (2 * dz + 6 + sp)
+            if r > 0:
+                top = row[out].max() if np.any(out) else -np.inf
+                lqo = -np.inf  # log q_out
+                if top > -np.inf:
+                    do = np.where(out, (row - top) / T, -np.inf)
+                    eo = np.exp(do)
+                    lqo = (top - row.max()) / T + np.log(eo.sum()) - np.log(e.sum())
+                L += r * ((np.log(r) if kind == "forward" else 0.0) - lqo)
+                if lqo > -np.inf:
+                    dz = np.where(out, np.where(eo > 0, -do, 0.0), dz)
+                    spo = 33 + 2 * (dz * eo)[out].sum() / eo.sum()
+                    serr += r * (sp + spo)
+                    off = np.where(out, r * eo / eo.sum(), 0.0)
+                    g = g - off
+                    gerr = gerr + off * (2 * dz + 6 + spo)
+                else:
+                    g = np.where(out, 0.0, g)
+            P = np.zeros(V)
+            np.add.at(P, i, p)
+            per[n, k] = L
+            step_err[n, k] = serr
+            grad[n, k] = f * (g - P)
+            grad_err[n, k] = abs(f) * (gerr + 3 * P)
+            # float32 exponentials below 2^-126 of their sum's largest are 0; the
+            # coefficient before them is at most f (W + r)
+            grad_unit[n, k] = abs(f) * (W + r)
+    return dict(per_step=per, loss=scale * per.mean(axis=1).sum(), grad=grad, step_err=step_err, grad_err=grad_err,
+                grad_unit=grad_unit)
+
+
+def verify_probs_ref(target, draft, ids, u, us, lens=None):
+    """target [B, K+1, V], draft [B, K, V] or None (one-hot), float64.  Returns
+    accept_len, emitted, overlap, and margin: the distance of u' Z from the
+    nearest step of the cumulative sum, relative to Z."""
+    p = np.asarray(target, dtype=np.float64)
+    B, K1, V = p.shape
+    K = K1 - 1
+    acc = np.full(B, -1, np.int32)
+    em = np.full((B, K + 1), -1, np.int32)
+    ov = np.full((B, K), np.nan)
+    margin = np.full(B, np.inf)
+
+    def good(x):
+        return bool(np.all(np.isfinite(x)) and np.all(x >= 0))
+
+    for b in range(B):
+        L = K if lens is None else int(lens[b])
+        if L < 0 or L > K or not 0 <= us[b] <= 1:
+            continue
+        x = np.asarray(ids[b, :L])
+        if np.any(x < 0) or np.any(x >= V) or not np.all((u[b, :L] >= 0) & (u[b, :L] <= 1)):
+            continue
+        px = p[b, np.arange(L), x]
+        qx = np.ones(L) if draft is None else np.asarray(draft[b, np.arange(L), x], dtype=np.float64)
+        if not (good(px) and good(qx)):
+            continue
+        n = 0
+        while n < L and np.float64(u[b, n]) * qx[n] < px[n]:
+            n += 1
+        pn = p[b, n]
+        r = pn
+        if n < L:
+            if draft is None:
+                qn = np.zeros(V)
+                r = pn.copy()
+                r[x[n]] = 0.0
+            else:
+                qn = np.asarray(draft[b, n], dtype=np.float64)
+                if not good(qn):
+                    continue
+                r = np.maximum(pn - qn, 0.0)
+        if not good(pn):
+            continue
+        if r.sum() == 0.0:
+            r = pn
+        C = np.cumsum(r)
+        if not C[-1] > 0:
+            continue
+        above = np.nonzero(C > np.float64(us[b]) * C[-1])[0]
+        tok = above[0] if len(above) else np.nonzero(r > 0)[0][-1]
+        margin[b] = np.abs(C - np.float64(us[b]) * C[-1]).min() / C[-1] if 0 < us[b] < 1 else np.inf
+        acc[b] = n
+        em[b, :n] = x[:n]
+        em[b, n] = tok
+        ov[b] = 0.0
+        for i in range(L):
+            if draft is None:
+                ov[b, i] = px[i]
+            else:
+                qi = np.asarray(draft[b, i], dtype=np.float64)
+                ov[b, i] = np.minimum(p[b, i], qi).sum() if good(p[b, i]) and good(qi) else np.nan
+    return dict(accept_len=acc, emitted=em, overlap=ov, margin=margin)

@@ -60,6 +60,12 @@ VERIFY_EX_ARGTYPES = VERIFY_ARGTYPES + [ctypes.POINTER(SpecLaunch)]
 VERIFY_NOALLOC_ARGTYPES = VERIFY_ARGTYPES[:-3] + [_P]
 KL_ARGTYPES = [_P, _I64, _I64, _P, _I64, _I64, _I, _I, _I, _I, _F, _I, _F, _P, _P, _P, _P, _SZ, _P]
 KL_KINDS = {"forward": 0, "ce": 1, "reverse": 2}
+TOP_ARGTYPES = [_P, _I64, _I64, _I, _I, _I, _I, _I, _P, _F, _P, _P, _P, _P, _SZ, _P]
+DISTILL_ARGTYPES = [_P, _I64, _I64, _I, _I, _I, _I, _P, _P, _I64, _I64, _I, _P, _I64, _I64, _F, _I, _F,
+                    _P, _P, _P, _I, _P, _SZ, _P]
+DISTILL_KINDS = {"forward": 0, "ce": 1}
+PROBS_ARGTYPES = [_P, _I64, _I64, _P, _I64, _I64, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+SPEC_MAX_LIST = 256
 DIAG_COLUMNS = ("entropy_target", "entropy_draft", "max_p", "alpha_to", "alpha_rs", "alpha_p_gt_q", "alpha_q_ge_p")
 
 
@@ -124,6 +130,18 @@ def load_library():
         lib.spec_kl_workspace_size.argtypes = [_I, _I, _I, _I]
         lib.spec_kl_loss_fwd_bwd.restype = _I
         lib.spec_kl_loss_fwd_bwd.argtypes = KL_ARGTYPES
+        lib.spec_top_logits_workspace_size.restype = _SZ
+        lib.spec_top_logits_workspace_size.argtypes = [_I, _I, _I, _I, _I]
+        lib.spec_top_logits.restype = _I
+        lib.spec_top_logits.argtypes = TOP_ARGTYPES
+        lib.spec_distill_workspace_size.restype = _SZ
+        lib.spec_distill_workspace_size.argtypes = [_I, _I, _I, _I, _I]
+        lib.spec_distill_loss_fwd_bwd.restype = _I
+        lib.spec_distill_loss_fwd_bwd.argtypes = DISTILL_ARGTYPES
+        lib.spec_verify_probs_workspace_size.restype = _SZ
+        lib.spec_verify_probs_workspace_size.argtypes = [_I, _I, _I, _I]
+        lib.spec_verify_probs.restype = _I
+        lib.spec_verify_probs.argtypes = PROBS_ARGTYPES
         _lib = lib
         return lib
 
@@ -524,3 +542,226 @@ def kl_loss_fwd_bwd(target_logits, draft_logits, temperature=1.0, kind="forward"
     if st != 0:
         raise SpecError("spec_kl_loss_fwd_bwd", st)
     return loss, per_step, grad
+
+
+# ---- records, distillation and verification from probabilities (specverify_rollout.h) ----
+#
+# These calls take their scratch memory from torch's allocator on the current
+# stream unless `ws` is given: calls on several streams, and graphs captured one
+# after another, then never share any.
+
+def top_logits_workspace_size(N, K, V, M, dtype=torch.bfloat16):
+    code = SPEC_BF16 if dtype == torch.bfloat16 else SPEC_F32
+    return int(load_library().spec_top_logits_workspace_size(N, K, V, M, code))
+
+
+def distill_workspace_size(N, K, V, M, dtype=torch.bfloat16):
+    code = SPEC_BF16 if dtype == torch.bfloat16 else SPEC_F32
+    return int(load_library().spec_distill_workspace_size(N, K, V, M, code))
+
+
+def verify_probs_workspace_size(B, K, V, dtype=torch.float32):
+    code = SPEC_BF16 if dtype == torch.bfloat16 else SPEC_F32
+    return int(load_library().spec_verify_probs_workspace_size(B, K, V, code))
+
+
+def _check_tensor(t, name, dtype, shape, device):
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s, got %s %s" % (
+            name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    if t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+
+
+def _gpu(t, name):
+    if not t.is_cuda:
+        raise ValueError("%s must be on a GPU" % name)
+    return t.device
+
+
+def _call(name, fn, need, ws, dev, args):
+    """fn(*args, workspace, size, stream) on the device of the tensors."""
+    if need == 0:
+        raise ValueError("%s: unsupported shape" % name)
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _call(name, fn, need, ws, dev, args)
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on %s" % dev)
+    st = fn(*args, ws.data_ptr(), ws.numel() * ws.element_size(), torch.cuda.current_stream(dev).cuda_stream)
+    if st != 0:
+        raise SpecError(name, st)
+
+
+def top_logits(logits, k, temperature=1.0, want_logz=True, ws=None, out=None):
+    """The k largest logits of every row and its log partition function
+    (spec_top_logits): the compact record of a target row that
+    :func:`distill_loss_fwd_bwd` trains on.
+
+    logits [R, V] or [N, K, V] (bf16 or f32, vocabulary dimension contiguous,
+    any other strides); 1 <= k <= 256; temperature: float, or a float32 tensor
+    of one value per row of the first dimension (it scales logz only).  Returns
+    a dict with ids [..., k] int32, values [..., k] float32 (largest first,
+    ties to the lowest index; -1 and -inf where a row has fewer than k logits
+    above -inf) and, with want_logz, logz [...] float32.  `out` takes such a
+    dict of contiguous tensors.
+    """
+    lib = load_library()
+    if logits.dim() not in (2, 3) or logits.stride(-1) != 1:
+        raise ValueError("logits must be [R, V] or [N, K, V] with a contiguous vocabulary dimension")
+    dev = _gpu(logits, "logits")
+    lead = logits.shape[:-1]
+    N, V = logits.shape[0], logits.shape[-1]
+    K, sk = (logits.shape[1], logits.stride(1)) if logits.dim() == 3 else (1, 0)
+    M = int(k)
+    t_ptr, t_scalar = _temperature_arg(temperature, N)
+    if t_ptr is not None and temperature.device != dev:
+        raise ValueError("temperature is on %s, expected %s" % (temperature.device, dev))
+    code = _dtype_code(logits)
+    if not 1 <= M <= SPEC_MAX_LIST:
+        raise ValueError("k must lie in [1, %d], got %d" % (SPEC_MAX_LIST, M))
+    if out is None:
+        out = {"ids": torch.empty(lead + (M,), dtype=torch.int32, device=dev),
+               "values": torch.empty(lead + (M,), dtype=torch.float32, device=dev)}
+        if want_logz:
+            out["logz"] = torch.empty(lead, dtype=torch.float32, device=dev)
+    else:
+        _check_tensor(out["ids"], "out['ids']", torch.int32, lead + (M,), dev)
+        _check_tensor(out["values"], "out['values']", torch.float32, lead + (M,), dev)
+        if "logz" in out:
+            _check_tensor(out["logz"], "out['logz']", torch.float32, lead, dev)
+    lz = out.get("logz")
+    _call("spec_top_logits", lib.spec_top_logits, lib.spec_top_logits_workspace_size(N, K, V, M, code), ws, dev,
+          (logits.data_ptr(), logits.stride(0), sk, code, N, K, V, M, t_ptr, t_scalar,
+           out["ids"].data_ptr(), out["values"].data_ptr(), None if lz is None else lz.data_ptr()))
+    return out
+
+
+def distill_loss_fwd_bwd(draft_logits, teacher_ids, teacher_values, teacher_logz=None, temperature=1.0,
+                         kind="forward", scale=1.0, want_grad=True, want_per_step=True, grad_dtype=None, ws=None,
+                         grad_out=None):
+    """Distillation of the draft from a teacher's top logits, loss and gradient
+    (spec_distill_loss_fwd_bwd).
+
+    draft_logits [N, K, V] (bf16 or f32); teacher_ids [N, K, M] int32 and
+    teacher_values [N, K, M] float32 (the same strides, the lists contiguous;
+    ids < 0 are unused entries); teacher_logz [N, K] float32 at the same
+    temperature, or None: with it the mass outside the list is one more
+    outcome, without it the list is renormalised.  kind in DISTILL_KINDS.
+    grad_dtype: torch.float32 (default) or the draft logits' dtype.
+    Returns (loss [1], per_step [N, K] or None, grad [N, K, V] or None); a
+    position without entries has no loss and a gradient of zeros.
+    """
+    lib = load_library()
+    if draft_logits.dim() != 3:
+        raise ValueError("draft_logits must be [N, K, V]")
+    N, K, V = draft_logits.shape
+    _check_rows(draft_logits, "draft_logits", (N, K, V))
+    dev = _gpu(draft_logits, "draft_logits")
+    code = _dtype_code(draft_logits)
+    if teacher_ids.dim() != 3 or teacher_ids.shape[0] != N or teacher_ids.shape[1] != K:
+        raise ValueError("teacher_ids must be [N, K, M] with N=%d, K=%d" % (N, K))
+    M = teacher_ids.shape[2]
+    if not 1 <= M <= SPEC_MAX_LIST:
+        raise ValueError("lists must have 1 to %d entries, got %d" % (SPEC_MAX_LIST, M))
+    if teacher_ids.dtype != torch.int32 or teacher_values.dtype != torch.float32:
+        raise ValueError("teacher_ids must be int32 and teacher_values float32")
+    if teacher_values.shape != teacher_ids.shape or teacher_values.stride()[:2] != teacher_ids.stride()[:2]:
+        raise ValueError("teacher_values must have the shape and strides of teacher_ids")
+    if M > 1 and (teacher_ids.stride(2) != 1 or teacher_values.stride(2) != 1):
+        raise ValueError("teacher_ids, teacher_values: the list dimension must be contiguous")
+    zp, zn, zk = None, 0, 0
+    if teacher_logz is not None:
+        if teacher_logz.dtype != torch.float32 or tuple(teacher_logz.shape) != (N, K):
+            raise ValueError("teacher_logz must be a float32 [N, K] tensor")
+        zp, zn, zk = teacher_logz.data_ptr(), teacher_logz.stride(0), teacher_logz.stride(1)
+    for t, name in ((teacher_ids, "teacher_ids"), (teacher_values, "teacher_values"), (teacher_logz, "teacher_logz")):
+        if t is not None and t.device != dev:
+            raise ValueError("%s is on %s, expected %s" % (name, t.device, dev))
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    per_step = torch.empty((N, K), dtype=torch.float32, device=dev) if want_per_step else None
+    grad, gcode = None, SPEC_F32
+    if want_grad:
+        if grad_dtype is None:
+            grad_dtype = torch.float32 if grad_out is None else grad_out.dtype
+        if grad_dtype not in (torch.float32, draft_logits.dtype):
+            raise TypeError("grad_dtype must be float32 or the draft logits' dtype, got %s" % grad_dtype)
+        gcode = SPEC_BF16 if grad_dtype == torch.bfloat16 else SPEC_F32
+        if grad_out is None:
+            grad = torch.empty((N, K, V), dtype=grad_dtype, device=dev)
+        else:
+            grad = grad_out
+            _check_tensor(grad, "grad_out", grad_dtype, draft_logits.shape, dev)
+            a0, a1 = grad.data_ptr(), grad.data_ptr() + grad.numel() * grad.element_size()
+            b0 = draft_logits.data_ptr()
+            b1 = b0 + ((N - 1) * draft_logits.stride(0) + (K - 1) * draft_logits.stride(1) + V) \
+                * draft_logits.element_size()
+            if a0 < b1 and b0 < a1:
+                raise ValueError("grad_out overlaps draft_logits")
+    _call("spec_distill_loss_fwd_bwd", lib.spec_distill_loss_fwd_bwd,
+          lib.spec_distill_workspace_size(N, K, V, M, code), ws, dev,
+          (draft_logits.data_ptr(), draft_logits.stride(0), draft_logits.stride(1), code, N, K, V,
+           teacher_ids.data_ptr(), teacher_values.data_ptr(), teacher_ids.stride(0), teacher_ids.stride(1), M,
+           zp, zn, zk, float(temperature), DISTILL_KINDS[kind] if isinstance(kind, str) else int(kind), float(scale),
+           loss.data_ptr(), None if per_step is None else per_step.data_ptr(),
+           None if grad is None else grad.data_ptr(), gcode))
+    return loss, per_step, grad
+
+
+def verify_probs(target_probs, draft_probs, draft_ids, accept_uniforms, sample_uniforms, draft_lens=None,
+                 want_overlap=True, ws=None, out=None):
+    """Chain rejection-sampling verification from given probabilities and
+    uniforms (spec_verify_probs).
+
+    target_probs [B, K+1, V], draft_probs [B, K, V] (bf16 or f32, same dtype,
+    vocabulary dimension contiguous) or None: one-hot drafts; draft_ids [B, K]
+    int32; accept_uniforms [B, K] and sample_uniforms [B] float32 in [0, 1];
+    draft_lens [B] int32 (drafts of each row, 0 to K) or None.  Returns a dict
+    with accept_len [B], emitted [B, K+1] (int32) and, unless want_overlap is
+    False, overlap [B, K]; without the overlaps only the emitting step's rows
+    are read.  K = 0 (no drafts) samples one token a row.
+    """
+    lib = load_library()
+    if target_probs.dim() != 3:
+        raise ValueError("target_probs must be [B, K+1, V]")
+    B, K1, V = target_probs.shape
+    K = K1 - 1
+    _check_rows(target_probs, "target_probs", (B, K1, V))
+    dev = _gpu(target_probs, "target_probs")
+    code = _dtype_code(target_probs)
+    dp, db, dk = None, 0, 0
+    if draft_probs is not None:
+        _check_rows(draft_probs, "draft_probs", (B, K, V))
+        if draft_probs.dtype != target_probs.dtype:
+            raise TypeError("target and draft probabilities must share a dtype")
+        if draft_probs.device != dev:
+            raise ValueError("draft_probs is on %s, expected %s" % (draft_probs.device, dev))
+        if K > 0:
+            dp, db, dk = draft_probs.data_ptr(), draft_probs.stride(0), draft_probs.stride(1)
+    ip = up = lp = None
+    if K > 0:
+        _check_tensor(draft_ids, "draft_ids", torch.int32, (B, K), dev)
+        _check_tensor(accept_uniforms, "accept_uniforms", torch.float32, (B, K), dev)
+        ip, up = draft_ids.data_ptr(), accept_uniforms.data_ptr()
+    _check_tensor(sample_uniforms, "sample_uniforms", torch.float32, (B,), dev)
+    if draft_lens is not None:
+        _check_tensor(draft_lens, "draft_lens", torch.int32, (B,), dev)
+        lp = draft_lens.data_ptr()
+    if out is None:
+        out = {"accept_len": torch.empty(B, dtype=torch.int32, device=dev),
+               "emitted": torch.empty((B, K + 1), dtype=torch.int32, device=dev)}
+        if want_overlap:
+            out["overlap"] = torch.empty((B, K), dtype=torch.float32, device=dev)
+    else:
+        _check_tensor(out["accept_len"], "out['accept_len']", torch.int32, (B,), dev)
+        _check_tensor(out["emitted"], "out['emitted']", torch.int32, (B, K + 1), dev)
+        if "overlap" in out:
+            _check_tensor(out["overlap"], "out['overlap']", torch.float32, (B, K), dev)
+    ov = out.get("overlap")
+    _call("spec_verify_probs", lib.spec_verify_probs, lib.spec_verify_probs_workspace_size(B, K, V, code), ws, dev,
+          (target_probs.data_ptr(), target_probs.stride(0), target_probs.stride(1), dp, db, dk, code, B, K, V,
+           ip, up, sample_uniforms.data_ptr(), lp, out["accept_len"].data_ptr(), out["emitted"].data_ptr(),
+           None if ov is None or K == 0 else ov.data_ptr()))
+    return out

@@ -17,9 +17,9 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libspecverify.so")
 ARCH = "gfx950"
 
-SOURCES = ["specverify.hip"]
+SOURCES = ["specverify.hip", "rollout.hip"]
 HEADERS = ["sv_device.h", "verify_kernel.h", "tv_kernel.h", "variants_kernel.h", "gumbel_kernel.h", "kl_kernel.h",
-           "fused_kernel.h", "resident_kernel.h"]
+           "fused_kernel.h", "resident_kernel.h", "sv_host.h", "top_kernel.h", "distill_kernel.h", "probs_kernel.h"]
 
 
 def hipcc():

@@ -1,0 +1,383 @@
+// probs_kernel.h — chain rejection-sampling verification from given
+// probabilities and given uniforms (paper Sec. 2.2 Eq. reject_sample, App.
+// G.1 Alg. rs_multinomial), in two launches:
+//
+//   1 probs_pass    one wave per (batch row, sub-chunk) of the emitting step,
+//                   with overlaps per (batch row, step, sub-chunk): the accept
+//                   tests from the gathered p(x_i), q(x_i), then the
+//                   sub-chunk's sums of max(0, p - q) and min(p, q).
+//   2 probs_finish  one workgroup per batch row: the sub-chunk in which the
+//                   residual's cumulative sum passes u' Z, that sub-chunk
+//                   again, the token.
+//
+// With the probabilities given, the accept tests need two gathered values a
+// step, so only the emitting step's pair (or the bonus row) is streamed.  What
+// bounds the pass is that read.
+//
+// The accept test u q < p is exact: u and q have 24-bit significands, so their
+// product is exact in float64.  p - q and every sum of the residual are
+// float64, so that a token depends on the order of the sums only where u' Z lies
+// within about 1e-15 Z of a step of the cumulative sum.
+#pragma once
+
+#include "sv_device.h"
+
+namespace sv {
+
+constexpr int kProbsVec = 16;  // vectors per lane of a sub-chunk (one wave)
+
+template <class E>
+constexpr int probs_sub() { return kProbsVec * 64 * E::EPV; }
+
+struct ProbsArgs {
+  const void* p; int64_t psb, psk;  // target probabilities [B, K + 1, V]
+  const void* q; int64_t qsb, qsk;  // draft probabilities [B, K, V], or nullptr: one-hot drafts
+  const int32_t* ids;               // [B, K]
+  const float* ua;                  // [B, K]
+  const float* us;                  // [B]
+  const int32_t* lens;              // [B] or nullptr
+  int B, K, V;
+  int C;                            // sub-chunks per row
+  int32_t* accept_len;
+  int32_t* emitted;
+  float* overlap;                   // [B, K] or nullptr
+  double* res;                      // [B][C] residual sums of the emitting step
+  double* ov;                       // [B][K][C] overlap sums (with overlap and draft probabilities)
+};
+
+// A probability as given: finite and not negative.
+__device__ __forceinline__ bool prob_ok(float p) { return p >= 0.f && p < INFINITY; }
+
+struct ProbsDecision {
+  int n, len;  // first rejected step (len if none), drafted tokens of the row
+  int x;       // the rejected token (n < len)
+  bool bad;    // a value the decision depends on is no probability, uniform, id or length
+  float px;    // lane i < len: p_i(x_i)
+};
+
+// The accept tests of one batch row, taken by a whole wave (lane i tests step i).
+template <class E>
+__device__ __forceinline__ ProbsDecision probs_decide(const ProbsArgs& a, int b) {
+  using raw = typename E::raw;
+  const int lane = threadIdx.x & 63;
+  ProbsDecision d;
+  d.len = a.lens ? a.lens[b] : a.K;
+  const bool len_bad = d.len < 0 || d.len > a.K;
+  if (len_bad) d.len = 0;
+  bool bad = len_bad, reject = false;
+  int x = 0;
+  d.px = 0.f;
+  if (lane < d.len) {
+    x = a.ids[static_cast<int64_t>(b) * a.K + lane];
+    const float u = a.ua[static_cast<int64_t>(b) * a.K + lane];
+    bad = x < 0 || x >= a.V;
+    const int xs = bad ? 0 : x;
+    const float p = E::one(static_cast<const raw*>(a.p) + b * a.psb + lane * a.psk + xs);
+    const float q = a.q ? E::one(static_cast<const raw*>(a.q) + b * a.qsb + lane * a.qsk + xs) : 1.f;
+    bad = bad || !(u >= 0.f && u <= 1.f) || !prob_ok(p) || !prob_ok(q);
+    reject = !(static_cast<double>(u) * static_cast<double>(q) < static_cast<double>(p));
+    d.px = p;
+  }
+  const float us = a.us[b];
+  bad = bad || !(us >= 0.f && us <= 1.f);
+  d.bad = __ballot(bad) != 0;
+  const uint64_t rej = __ballot(reject);
+  d.n = rej ? __builtin_ctzll(rej) : d.len;
+  d.x = __builtin_amdgcn_readlane(x, d.n < 63 ? d.n : 63);
+  return d;
+}
+
+// Load S vectors per lane as load_span does, with 0 beyond the row.
+template <class E, int S, int W>
+__device__ __forceinline__ void load_probs(const typename E::raw* __restrict__ row, int e0, int idx, int V,
+                                           float (&x)[S][E::EPV]) {
+  load_span<E, S, W>(row, e0, idx, V, x);
+  if (e0 + S * W * E::EPV > V) {
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+      const int v0 = e0 + (j * W + idx) * E::EPV;
+#pragma unroll
+      for (int k = 0; k < E::EPV; ++k)
+        if (v0 + k >= V) x[j][k] = 0.f;
+    }
+  }
+}
+
+// The residual of one element: max(0, p - q), with the rejected token of a
+// one-hot draft struck out by the caller (q = 0 everywhere else).
+__device__ __forceinline__ double residual(float p, float q) {
+  return fmax(static_cast<double>(p) - static_cast<double>(q), 0.0);
+}
+
+// Units of launch 1: without overlaps (row b, sub-chunk), with them (row b,
+// step i <= K, sub-chunk), i = K being the bonus row of a row whose drafts all
+// passed.
+template <class E, bool OV>
+__global__ __launch_bounds__(kThreads) void probs_pass_kernel(ProbsArgs a, int64_t units) {
+  using raw = typename E::raw;
+  constexpr int EPV = E::EPV, S = 4, SUB = probs_sub<E>();
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t g = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+  if (g >= units) return;
+  const int c = static_cast<int>(g % a.C);
+  const int64_t bi = g / a.C;
+  const int steps = OV ? a.K + 1 : 1;
+  const int b = static_cast<int>(bi / steps);
+  const ProbsDecision d = probs_decide<E>(a, b);
+  const int i = OV ? static_cast<int>(bi % steps) : d.n;
+  const bool emit = i == d.n;             // this unit sums the residual
+  const bool pair = OV && a.q && i < d.len;  // this unit sums the overlap
+  const bool draft = a.q != nullptr && i < d.len;
+  if (d.bad || !(emit || pair)) return;
+  const raw* prow = static_cast<const raw*>(a.p) + b * a.psb + i * a.psk;
+  const raw* qrow = draft ? static_cast<const raw*>(a.q) + b * a.qsb + i * a.qsk : prow;
+  const int struck = (!a.q && i < d.len) ? d.x : -1;
+  const int e0 = c * SUB;
+  double rs = 0.0, os = 0.0;
+  float lo = 0.f, hi = 0.f;
+#pragma unroll 1
+  for (int st = 0; st < kProbsVec / S; ++st) {
+    const int es = e0 + st * S * 64 * EPV;
+    if (es >= a.V) break;
+    float x[S][EPV], y[S][EPV];
+    load_probs<E, S, 64>(prow, es, lane, a.V, x);
+    if (draft) {
+      load_probs<E, S, 64>(qrow, es, lane, a.V, y);
+    } else {
+#pragma unroll
+      for (int j = 0; j < S; ++j)
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) y[j][k] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+      const int v0 = es + (j * 64 + lane) * EPV;
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) {
+        lo = __builtin_elementwise_minimum(lo, __builtin_elementwise_minimum(x[j][k], y[j][k]));
+        hi = __builtin_elementwise_maximum(hi, __builtin_elementwise_maximum(x[j][k], y[j][k]));
+        if (emit && v0 + k != struck) rs += residual(x[j][k], y[j][k]);
+        if (pair) os += static_cast<double>(fminf(x[j][k], y[j][k]));
+      }
+    }
+  }
+  if (!(lo >= 0.f && hi < INFINITY)) rs = os = __builtin_nan("");
+  rs = wave_sum(rs);
+  if (OV) os = wave_sum(os);
+  if (lane == 0) {
+    if (emit) a.res[static_cast<int64_t>(b) * a.C + c] = rs;
+    if (pair) a.ov[(static_cast<int64_t>(b) * a.K + i) * a.C + c] = os;
+  }
+}
+
+// Scratch of probs_finish.
+struct ProbsLds {
+  double wsum[4][kWaves];
+  double total;
+  RedLds<1> red;
+};
+
+// Exclusive prefix (in thread order) of one double per thread and the total.
+__device__ __forceinline__ double wg_excl_scan(double v, double* total, ProbsLds& s) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const double inc = wave_incl_scan(v);
+  if (lane == 63) s.wsum[0][wave] = inc;
+  __syncthreads();
+  double base = 0.0, tot = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w == wave) base = tot;
+    tot += s.wsum[0][w];
+  }
+  __syncthreads();
+  *total = tot;
+  const double ex = __shfl_up(inc, 1, 64);
+  return base + (lane ? ex : 0.0);
+}
+
+// The token of one sub-chunk: the first element v whose cumulative residual
+// (from `base` at the sub-chunk's start) exceeds `target`, else the last
+// element with residual (where rounding left none above), -1 if there is none.
+template <class E>
+__device__ __forceinline__ int probs_pick(const typename E::raw* prow, const typename E::raw* qrow, int struck, int V,
+                                          int c, double base, double target, ProbsLds& s) {
+  constexpr int EPV = E::EPV, TILES = probs_sub<E>() / (kThreads * EPV);
+  static_assert(TILES == 4, "one wsum row per tile");
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int e0 = c * probs_sub<E>();
+  float x[TILES][EPV], y[TILES][EPV];
+  load_probs<E, TILES, kThreads>(prow, e0, t, V, x);
+  if (qrow) {
+    load_probs<E, TILES, kThreads>(qrow, e0, t, V, y);
+  } else {
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) y[j][k] = 0.f;
+  }
+  double inc[TILES], own[TILES];
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    const int v0 = e0 + (j * kThreads + t) * EPV;
+    own[j] = 0.0;
+#pragma unroll
+    for (int k = 0; k < EPV; ++k) own[j] += v0 + k == struck ? 0.0 : residual(x[j][k], y[j][k]);
+    inc[j] = wave_incl_scan(own[j]);
+    if (lane == 63) s.wsum[j][wave] = inc[j];
+  }
+  __syncthreads();
+  int first = 0x7fffffff, last = -1;
+  double before = base;
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    double mine = before;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == wave) mine = before;
+      before += s.wsum[j][w];
+    }
+    const double ex = __shfl_up(inc[j], 1, 64);
+    double cum = mine + (lane ? ex : 0.0);
+    const int v0 = e0 + (j * kThreads + t) * EPV;
+#pragma unroll
+    for (int k = 0; k < EPV; ++k) {
+      const double r = v0 + k == struck ? 0.0 : residual(x[j][k], y[j][k]);
+      cum += r;
+      if (r > 0.0) {
+        last = v0 + k;
+        if (cum > target && v0 + k < first) first = v0 + k;
+      }
+    }
+  }
+  first = wg_min_int(first, s.red);
+  last = -wg_min_int(-last, s.red);
+  return first != 0x7fffffff ? first : last;
+}
+
+// Sum of sub-chunk c of a row (pair) as probs_pass forms it, by one wave; for
+// the rows whose residual has no mass, whose token is drawn from p itself.
+template <class E>
+__device__ __forceinline__ double probs_sub_sum(const typename E::raw* prow, int V, int c) {
+  constexpr int EPV = E::EPV, S = 4;
+  const int lane = threadIdx.x & 63;
+  double rs = 0.0;
+  float lo = 0.f, hi = 0.f;
+#pragma unroll 1
+  for (int st = 0; st < kProbsVec / S; ++st) {
+    const int es = c * probs_sub<E>() + st * S * 64 * EPV;
+    if (es >= V) break;
+    float x[S][EPV];
+    load_probs<E, S, 64>(prow, es, lane, V, x);
+#pragma unroll
+    for (int j = 0; j < S; ++j)
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) {
+        lo = __builtin_elementwise_minimum(lo, x[j][k]);
+        hi = __builtin_elementwise_maximum(hi, x[j][k]);
+        rs += static_cast<double>(x[j][k]);
+      }
+  }
+  if (!(lo >= 0.f && hi < INFINITY)) rs = __builtin_nan("");
+  return wave_sum(rs);
+}
+
+// The sub-chunk of a row in which the cumulative sum passes u Z: every thread
+// adds a run of consecutive sub-chunk sums.  Returns -1 where Z is 0 and -2
+// where a sum is NaN.
+__device__ __forceinline__ int probs_locate(const double* sums, int C, double u, double* base, double* target,
+                                            ProbsLds& s) {
+  const int t = threadIdx.x;
+  const int run = (C + kThreads - 1) / kThreads;
+  const int64_t lo = static_cast<int64_t>(t) * run;
+  double v = 0.0;
+  for (int64_t c = lo; c < lo + run && c < C; ++c) v += sums[c];
+  double z;
+  const double ex = wg_excl_scan(v, &z, s);
+  if (z != z) return -2;
+  if (!(z > 0.0)) return -1;
+  const double tg = u * z;
+  // the first sub-chunk whose cumulative sum exceeds the target, else the last with mass
+  int first = 0x7fffffff, last = -1;
+  double cum = ex;
+  for (int64_t c = lo; c < lo + run && c < C; ++c) {
+    const double m = sums[c];
+    cum += m;
+    if (m > 0.0) {
+      last = static_cast<int>(c);
+      if (cum > tg && first == 0x7fffffff) first = static_cast<int>(c);
+    }
+  }
+  first = wg_min_int(first, s.red);
+  last = -wg_min_int(-last, s.red);
+  const int at = first != 0x7fffffff ? first : last;
+  // the cumulative sum before it, from the thread whose run holds it
+  if (at / run == t) {
+    double cb = ex;
+    for (int64_t c = lo; c < at; ++c) cb += sums[c];
+    s.total = cb;
+  }
+  __syncthreads();
+  *base = s.total;
+  *target = tg;
+  __syncthreads();
+  return at;
+}
+
+template <class E>
+__global__ __launch_bounds__(kThreads) void probs_finish_kernel(ProbsArgs a) {
+  using raw = typename E::raw;
+  __shared__ ProbsLds s;
+  const int b = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const ProbsDecision d = probs_decide<E>(a, b);
+  const bool rejected = d.n < d.len;
+  int tok = -1;
+  if (!d.bad) {
+    const raw* prow = static_cast<const raw*>(a.p) + b * a.psb + d.n * a.psk;
+    const raw* qrow = (rejected && a.q) ? static_cast<const raw*>(a.q) + b * a.qsb + d.n * a.qsk : nullptr;
+    double* sums = a.res + static_cast<int64_t>(b) * a.C;
+    const double u = static_cast<double>(a.us[b]);
+    double base, target;
+    int struck = (rejected && !a.q) ? d.x : -1;
+    int c = probs_locate(sums, a.C, u, &base, &target, s);
+    if (c == -1 && rejected) {
+      // the residual has no mass: the token is drawn from p
+      for (int cc = wave; cc < a.C; cc += kWaves) {
+        const double v = probs_sub_sum<E>(prow, a.V, cc);
+        if (lane == 0) sums[cc] = v;
+      }
+      __syncthreads();
+      qrow = nullptr;
+      struck = -1;
+      c = probs_locate(sums, a.C, u, &base, &target, s);
+    }
+    if (c >= 0) tok = probs_pick<E>(prow, qrow, struck, a.V, c, base, target, s);
+  }
+  const bool bad = tok < 0;
+  if (t == 0) a.accept_len[b] = bad ? -1 : d.n;
+  if (t <= a.K) {
+    const int64_t o = static_cast<int64_t>(b) * (a.K + 1) + t;
+    int v = -1;
+    if (!bad && t == d.n) v = tok;
+    if (!bad && t < d.n) v = a.ids[static_cast<int64_t>(b) * a.K + t];
+    a.emitted[o] = v;
+  }
+  if (!a.overlap) return;
+  for (int i = wave; i < a.K; i += kWaves) {
+    float v;
+    if (bad) {
+      v = __builtin_nanf("");
+    } else if (i >= d.len) {
+      v = 0.f;
+    } else if (!a.q) {
+      v = __shfl(d.px, i, 64);
+    } else {
+      const double* o = a.ov + (static_cast<int64_t>(b) * a.K + i) * a.C;
+      double m = 0.0;
+      for (int c = lane; c < a.C; c += 64) m += o[c];
+      v = static_cast<float>(wave_sum(m));
+    }
+    if (lane == 0) a.overlap[static_cast<int64_t>(b) * a.K + i] = v;
+  }
+}
+
+}  // namespace sv

@@ -1,0 +1,295 @@
+// rollout.hip — argument validation, workspace layout and launch sequences of
+// the entry points declared in include/specverify_rollout.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <cstddef>
+#include <cstdint>
+
+#include "specverify_rollout.h"
+#include "sv_device.h"
+#include "sv_host.h"
+#include "distill_kernel.h"
+#include "probs_kernel.h"
+#include "top_kernel.h"
+
+namespace {
+
+using sv::align_up;
+using sv::aligned16;
+using sv::esize_of;
+using sv::extent_ok;
+
+static_assert(SPEC_MAX_LIST == sv::kTopMax && SPEC_MAX_LIST == sv::kListMax, "list length");
+
+bool dtype_ok(spec_dtype dt) { return dt == SPEC_F32 || dt == SPEC_BF16; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A launch holds fewer than 2^32 threads in all; workgroups have at least 256.
+constexpr int64_t kMaxGroups = int64_t{1} << 24;
+
+// Rows of V elements read in chunks of 16384, a workgroup each at most.
+bool rows_fit(int64_t rows, int V) {
+  return rows >= 1 && rows < (int64_t{1} << 31) && V >= 1 && V <= SPEC_MAX_V && rows * ceil_div(V, 16384) < kMaxGroups;
+}
+
+spec_status launched() { return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_EHIP; }
+
+dim3 groups(int64_t n) { return dim3(static_cast<unsigned>(n)); }
+
+// ---- top logits -------------------------------------------------------------------
+// Workgroups up to which rows are split, each part at least a load step.
+constexpr int64_t kTopGroups = 1024;
+
+struct TopPlan {
+  int P = 1, part = 0;
+  size_t cand = 0, stats = 0, total = 256;
+};
+TopPlan top_plan(int64_t R, int V, int M, spec_dtype dt) {
+  TopPlan p;
+  const int64_t step = int64_t{sv::kTopStep} * sv::kThreads * (dt == SPEC_BF16 ? sv::BF16::EPV : sv::F32::EPV);
+  const int64_t steps = ceil_div(V, step);
+  const int64_t parts = std::max<int64_t>(1, std::min(steps, kTopGroups / R));
+  const int64_t per = ceil_div(steps, parts);
+  p.P = static_cast<int>(ceil_div(steps, per));
+  p.part = static_cast<int>(std::min<int64_t>(per * step, V));
+  if (p.P > 1) {
+    size_t off = 0;
+    p.cand = off; off = align_up(off + static_cast<size_t>(R) * p.P * M * sizeof(uint64_t), 256);
+    p.stats = off; off = align_up(off + static_cast<size_t>(R) * p.P * sizeof(sv::RowStat), 256);
+    p.total = off;
+  }
+  return p;
+}
+
+bool top_sizes_ok(int N, int K, int V, int M) {
+  return N >= 1 && K >= 1 && M >= 1 && M <= SPEC_MAX_LIST && rows_fit(int64_t{N} * K, V);
+}
+
+template <class E, bool LZ>
+spec_status launch_top(const sv::TopArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((sv::top_part_kernel<E, LZ>), groups(a.R * a.P), dim3(sv::kThreads), 0, s, a);
+  if (a.P > 1) hipLaunchKernelGGL(sv::top_merge_kernel<LZ>, groups(a.R), dim3(sv::kThreads), 0, s, a);
+  return launched();
+}
+
+// ---- distillation -------------------------------------------------------------------
+struct DistillLayout {
+  size_t info = 0, stats = 0, part = 0, total = 0;
+  int C = 0;  // sub-chunks per row
+};
+DistillLayout distill_layout(int N, int K, int V, spec_dtype dt) {
+  DistillLayout L;
+  const size_t units = static_cast<size_t>(N) * K;
+  L.C = static_cast<int>(ceil_div(V, dt == SPEC_BF16 ? sv::distill_sub<sv::BF16>() : sv::distill_sub<sv::F32>()));
+  size_t off = 0;
+  L.info = off; off = align_up(off + units * sizeof(sv::ListInfo), 256);
+  L.stats = off; off = align_up(off + units * L.C * sizeof(sv::DistillStat), 256);
+  L.part = off; off = align_up(off + units * sizeof(double), 256);
+  L.total = off;
+  return L;
+}
+
+bool distill_sizes_ok(int N, int K, int V, int M) {
+  return N >= 1 && K >= 1 && K <= SPEC_MAX_K && M >= 1 && M <= SPEC_MAX_LIST && rows_fit(int64_t{N} * K, V);
+}
+
+// The gradient pass reads bfloat16 as 4-element vectors: a 16-byte float32
+// store per lane.
+template <class E> struct Quad { using type = E; };
+template <> struct Quad<sv::BF16> { using type = sv::BF16H; };
+
+template <class E, bool TAIL, class G>
+spec_status launch_distill(const sv::DistillArgs& a, hipStream_t s) {
+  const int64_t units = int64_t{a.N} * a.K, nsub = units * a.C;
+  const int64_t lists = ceil_div(units, sv::kWaves);
+  hipLaunchKernelGGL((sv::distill_stats_kernel<E, TAIL>), groups(lists + ceil_div(nsub, sv::kWaves)),
+                     dim3(sv::kThreads), 0, s, a, static_cast<int>(lists), nsub);
+  if (a.grad) {
+    const int CH = static_cast<int>(ceil_div(a.V, sv::kDistillChunk));
+    hipLaunchKernelGGL((sv::distill_grad_kernel<typename Quad<E>::type, G>), groups(units * CH), dim3(sv::kThreads), 0,
+                       s, a, CH);
+  } else {
+    hipLaunchKernelGGL(sv::distill_norm_kernel, groups(lists), dim3(sv::kThreads), 0, s, a);
+  }
+  hipLaunchKernelGGL(sv::distill_loss_kernel, dim3(1), dim3(sv::kThreads), 0, s, static_cast<const double*>(a.part),
+                     units, a.loss_scale, a.loss);
+  return launched();
+}
+
+template <class E, bool TAIL>
+spec_status launch_distill_grad(const sv::DistillArgs& a, spec_dtype gd, hipStream_t s) {
+  return gd == SPEC_BF16 ? launch_distill<E, TAIL, sv::GradBF16>(a, s) : launch_distill<E, TAIL, sv::GradF32>(a, s);
+}
+
+// ---- verification from probabilities --------------------------------------------------
+struct ProbsLayout {
+  size_t res = 0, ov = 0, total = 0;
+  int C = 0;
+};
+ProbsLayout probs_layout(int B, int K, int V, spec_dtype dt) {
+  ProbsLayout L;
+  L.C = static_cast<int>(ceil_div(V, dt == SPEC_BF16 ? sv::probs_sub<sv::BF16>() : sv::probs_sub<sv::F32>()));
+  size_t off = 0;
+  L.res = off; off = align_up(off + static_cast<size_t>(B) * L.C * sizeof(double), 256);
+  L.ov = off; off = align_up(off + static_cast<size_t>(B) * K * L.C * sizeof(double), 256);
+  L.total = off;
+  return L;
+}
+
+bool probs_sizes_ok(int B, int K, int V) {
+  return B >= 1 && K >= 0 && K <= SPEC_MAX_K && V >= 1 && V <= SPEC_MAX_V &&
+         int64_t{B} * (K + 1) * ceil_div(V, 4096) < kMaxGroups * sv::kWaves && B < kMaxGroups;
+}
+
+template <class E>
+spec_status launch_probs(const sv::ProbsArgs& a, hipStream_t s) {
+  if (a.overlap) {
+    const int64_t units = int64_t{a.B} * (a.K + 1) * a.C;
+    hipLaunchKernelGGL((sv::probs_pass_kernel<E, true>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads), 0, s,
+                       a, units);
+  } else {
+    const int64_t units = int64_t{a.B} * a.C;
+    hipLaunchKernelGGL((sv::probs_pass_kernel<E, false>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads), 0, s,
+                       a, units);
+  }
+  hipLaunchKernelGGL(sv::probs_finish_kernel<E>, groups(a.B), dim3(sv::kThreads), 0, s, a);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t spec_top_logits_workspace_size(int N, int K, int V, int M, spec_dtype dtype) {
+  if (!dtype_ok(dtype) || !top_sizes_ok(N, K, V, M)) return 0;
+  return top_plan(int64_t{N} * K, V, M, dtype).total;
+}
+
+spec_status spec_top_logits(const void* logits, int64_t stride_n, int64_t stride_k, spec_dtype dtype, int N, int K,
+                            int V, int M, const float* temperature, float temperature_scalar, int32_t* ids,
+                            float* values, float* logz, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype) || M > SPEC_MAX_LIST) return SPEC_EUNSUPPORTED;
+  if (!top_sizes_ok(N, K, V, M)) return SPEC_EINVAL;
+  if (!logits || !ids || !values) return SPEC_EINVAL;
+  if (stride_n < 0 || stride_k < 0) return SPEC_EINVAL;
+  if (!extent_ok(logits, N, stride_n, K, stride_k, V, esize_of(dtype))) return SPEC_EINVAL;
+  if (!temperature && !(temperature_scalar > 0.f && std::isfinite(temperature_scalar))) return SPEC_EINVAL;
+  const TopPlan p = top_plan(int64_t{N} * K, V, M, dtype);
+  if (!workspace || workspace_bytes < p.total) return SPEC_EWORKSPACE;
+  if (!aligned16(workspace)) return SPEC_EINVAL;
+
+  sv::TopArgs a{};
+  a.rows.tgt = logits; a.rows.tsb = stride_n; a.rows.tsk = stride_k; a.rows.tper = K;
+  a.rows.dper = 1;
+  a.rows.nb = N;
+  a.rows.temp = temperature; a.rows.temp_scalar = temperature_scalar;
+  a.rows.V = V;
+  a.R = int64_t{N} * K;
+  a.M = M; a.P = p.P; a.part = p.part;
+  a.ids = ids; a.values = values; a.logz = logz;
+  char* ws = static_cast<char*>(workspace);
+  a.cand = reinterpret_cast<uint64_t*>(ws + p.cand);
+  a.stats = reinterpret_cast<sv::RowStat*>(ws + p.stats);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == SPEC_BF16) return logz ? launch_top<sv::BF16, true>(a, s) : launch_top<sv::BF16, false>(a, s);
+  return logz ? launch_top<sv::F32, true>(a, s) : launch_top<sv::F32, false>(a, s);
+}
+
+size_t spec_distill_workspace_size(int N, int K, int V, int M, spec_dtype dtype) {
+  if (!dtype_ok(dtype) || !distill_sizes_ok(N, K, V, M)) return 0;
+  return distill_layout(N, K, V, dtype).total;
+}
+
+spec_status spec_distill_loss_fwd_bwd(const void* draft_logits, int64_t d_stride_n, int64_t d_stride_k,
+                                      spec_dtype dtype, int N, int K, int V, const int32_t* teacher_ids,
+                                      const float* teacher_values, int64_t l_stride_n, int64_t l_stride_k, int M,
+                                      const float* teacher_logz, int64_t z_stride_n, int64_t z_stride_k,
+                                      float temperature, spec_distill_kind kind, float scale, float* loss,
+                                      float* per_step, void* grad_draft, spec_dtype grad_dtype, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype) || K > SPEC_MAX_K || M > SPEC_MAX_LIST) return SPEC_EUNSUPPORTED;
+  if (grad_draft && grad_dtype != SPEC_F32 && grad_dtype != dtype) return SPEC_EUNSUPPORTED;
+  if (!distill_sizes_ok(N, K, V, M)) return SPEC_EINVAL;
+  if (!draft_logits || !teacher_ids || !teacher_values || !loss) return SPEC_EINVAL;
+  if (d_stride_n < 0 || d_stride_k < 0 || l_stride_n < 0 || l_stride_k < 0) return SPEC_EINVAL;
+  if (teacher_logz && (z_stride_n < 0 || z_stride_k < 0)) return SPEC_EINVAL;
+  if (!extent_ok(draft_logits, N, d_stride_n, K, d_stride_k, V, esize_of(dtype)) ||
+      !extent_ok(teacher_ids, N, l_stride_n, K, l_stride_k, M, sizeof(int32_t)) ||
+      !extent_ok(teacher_values, N, l_stride_n, K, l_stride_k, M, sizeof(float)) ||
+      (teacher_logz && !extent_ok(teacher_logz, N, z_stride_n, K, z_stride_k, 1, sizeof(float))))
+    return SPEC_EINVAL;
+  if (!(temperature > 0.f && std::isfinite(temperature))) return SPEC_EINVAL;
+  if (kind != SPEC_DISTILL_FORWARD && kind != SPEC_DISTILL_CE) return SPEC_EINVAL;
+  if (!std::isfinite(scale)) return SPEC_EINVAL;
+  const DistillLayout L = distill_layout(N, K, V, dtype);
+  if (!workspace || workspace_bytes < L.total) return SPEC_EWORKSPACE;
+  if (!aligned16(workspace)) return SPEC_EINVAL;
+
+  sv::DistillArgs a{};
+  a.z = draft_logits; a.zsn = d_stride_n; a.zsk = d_stride_k;
+  a.ids = teacher_ids; a.vals = teacher_values; a.lsn = l_stride_n; a.lsk = l_stride_k;
+  a.logz = teacher_logz; a.osn = z_stride_n; a.osk = z_stride_k;
+  a.N = N; a.K = K; a.V = V; a.M = M; a.C = L.C;
+  a.kind = kind == SPEC_DISTILL_FORWARD ? sv::kDistillForward : sv::kDistillCe;
+  // log2(e) / T as a float below it and a positive remainder
+  const double sc = std::min(sv::kLog2eD / static_cast<double>(temperature), static_cast<double>(FLT_MAX));
+  a.s_hi = static_cast<float>(sc);
+  if (static_cast<double>(a.s_hi) > sc) a.s_hi = std::nextafter(a.s_hi, 0.f);
+  a.s_lo = std::max(static_cast<float>(sc - static_cast<double>(a.s_hi)), FLT_TRUE_MIN);
+  a.inv_t = 1.0 / static_cast<double>(temperature);
+  a.loss_scale = static_cast<double>(scale) / K;
+  a.f = a.loss_scale * a.inv_t;
+  a.loss = loss; a.per_step = per_step; a.grad = grad_draft;
+  char* ws = static_cast<char*>(workspace);
+  a.info = reinterpret_cast<sv::ListInfo*>(ws + L.info);
+  a.stats = reinterpret_cast<sv::DistillStat*>(ws + L.stats);
+  a.part = reinterpret_cast<double*>(ws + L.part);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool tail = teacher_logz != nullptr;
+  if (dtype == SPEC_BF16)
+    return tail ? launch_distill_grad<sv::BF16, true>(a, grad_dtype, s)
+                : launch_distill_grad<sv::BF16, false>(a, grad_dtype, s);
+  return tail ? launch_distill<sv::F32, true, sv::GradF32>(a, s) : launch_distill<sv::F32, false, sv::GradF32>(a, s);
+}
+
+size_t spec_verify_probs_workspace_size(int B, int K, int V, spec_dtype dtype) {
+  if (!dtype_ok(dtype) || !probs_sizes_ok(B, K, V)) return 0;
+  return probs_layout(B, K, V, dtype).total;
+}
+
+spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int64_t t_stride_k,
+                              const void* draft_probs, int64_t d_stride_b, int64_t d_stride_k, spec_dtype dtype,
+                              int B, int K, int V, const int32_t* draft_ids, const float* accept_uniforms,
+                              const float* sample_uniforms, const int32_t* draft_lens, int32_t* accept_len,
+                              int32_t* emitted_ids, float* overlap, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  if (!dtype_ok(dtype) || K > SPEC_MAX_K) return SPEC_EUNSUPPORTED;
+  if (!probs_sizes_ok(B, K, V)) return SPEC_EINVAL;
+  if (!target_probs || !sample_uniforms || !accept_len || !emitted_ids) return SPEC_EINVAL;
+  if (K > 0 && (!draft_ids || !accept_uniforms)) return SPEC_EINVAL;
+  if (t_stride_b < 0 || t_stride_k < 0 || (draft_probs && (d_stride_b < 0 || d_stride_k < 0))) return SPEC_EINVAL;
+  if (!extent_ok(target_probs, B, t_stride_b, K + 1, t_stride_k, V, esize_of(dtype)) ||
+      (draft_probs && K > 0 && !extent_ok(draft_probs, B, d_stride_b, K, d_stride_k, V, esize_of(dtype))))
+    return SPEC_EINVAL;
+  const ProbsLayout L = probs_layout(B, K, V, dtype);
+  if (!workspace || workspace_bytes < L.total) return SPEC_EWORKSPACE;
+  if (!aligned16(workspace)) return SPEC_EINVAL;
+
+  sv::ProbsArgs a{};
+  a.p = target_probs; a.psb = t_stride_b; a.psk = t_stride_k;
+  a.q = draft_probs; a.qsb = d_stride_b; a.qsk = d_stride_k;
+  a.ids = draft_ids; a.ua = accept_uniforms; a.us = sample_uniforms; a.lens = draft_lens;
+  a.B = B; a.K = K; a.V = V; a.C = L.C;
+  a.accept_len = accept_len; a.emitted = emitted_ids;
+  a.overlap = K > 0 ? overlap : nullptr;
+  char* ws = static_cast<char*>(workspace);
+  a.res = reinterpret_cast<double*>(ws + L.res);
+  a.ov = reinterpret_cast<double*>(ws + L.ov);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return dtype == SPEC_BF16 ? launch_probs<sv::BF16>(a, s) : launch_probs<sv::F32>(a, s);
+}
+
+}  // extern "C"
