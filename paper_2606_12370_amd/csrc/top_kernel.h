@@ -1,39 +1,45 @@
 // top_kernel.h — the M largest logits of every row, largest first with ties to
 // the lowest index, and the row's log partition function, each logit read once.
 //
-// A workgroup streams its part of a row with a threshold below which no logit
-// can be among the part's M largest, and collects what exceeds it in LDS:
+// A workgroup streams its part of a row and keeps, in LDS, one 64-bit key per
+// vector of logits (eight bfloat16, four float32) that can still matter: the
+// order of the vector's largest logit in the high half, the reversed vector index
+// in the low half.  The M largest keys name the vectors that hold the M largest
+// logits: a logit outside them has M vectors before it, each with a logit that is
+// larger, or equal at a lower index.  So
 //
-//   - every candidate is one 64-bit key, the logit's order in the high half and
-//     the reversed index in the low half, so that keys are distinct and "the M
-//     largest keys" settles ties;
-//   - the first load step bounds the threshold by the M-th largest of the 256
-//     threads' own maxima (at least M logits are as large).  Later logits have
-//     larger indices, so they must exceed it;
-//   - where the candidates outgrow the buffer, a radix selection keeps the M
-//     largest keys and raises the threshold to the least of them.
+//   - a step adds the vectors whose largest logit exceeds the threshold (later
+//     vectors have larger indices, so a tie with it cannot matter);
+//   - where the keys outgrow twice the list's length, a radix selection keeps
+//     the M largest and raises the threshold: a row of random order then adds
+//     about M / s keys in step s, a row in ascending order all of its vectors;
+//   - at the end the last M vectors are read again, and their logits sorted.
 //
-// A row of random order passes a few hundred candidates; a row in ascending
-// order selects once per tile of 256 vectors and stays right.  Calls of few
-// rows split each row over several workgroups, whose lists a second launch
-// merges with the same buffer.  The pass is bound by its one read of the
-// logits and, close behind, by the vector instructions of the log partition
-// (an exponential, a fused multiply-add and an add per logit).
+// Keys of vectors instead of logits make the frequent part one compare and, per
+// wave, four ballots a step (candidate logits taken one by one where they occur,
+// trimmed by ranking, took 14 of the pass's 17 thousand vector instructions a
+// wave; R = 12288, V = 151936 bfloat16, M = 128: 1392 us).  Calls of few rows
+// split each row over several workgroups, whose lists a second launch merges.
 #pragma once
 
 #include "sv_device.h"
 
 namespace sv {
 
-constexpr int kTopMax = 256;  // longest list
-// tiles per load step
-constexpr int kTopStep = 4;
-// Candidates held: the list and one tile of 256 16-byte bfloat16 vectors, so
-// that a selection always makes room for a tile.
-constexpr int kTopCap = kTopMax + 2048;
-// Candidates up to which the list is sorted without a selection before
-// (each thread ranks two keys).
+constexpr int kTopMax = 256;   // longest list
+constexpr int kTopStep = 4;    // tiles per load step
+constexpr int kTopStepVecs = kTopStep * kThreads;
+// Keys held: twice the longest list and its slack and one step's vectors; at the
+// end eight logits of each of M vectors.
+constexpr int kTopCap = 2048;
+// Keys beyond twice the list's length from which they are trimmed.
+constexpr int kTopSlack = 64;
+// Keys up to which a list is sorted by ranking every key against every other
+// (two keys a thread); more are thinned by a selection before.
 constexpr int kTopRank = 512;
+constexpr int kTopWaves = 6;   // waves per SIMD that the registers allow
+static_assert(2 * kTopMax + kTopSlack + kTopStepVecs <= kTopCap, "room for a step's vectors");
+static_assert(kTopMax * 8 <= kTopCap, "room for the last vectors' logits");
 
 struct TopArgs {
   RowsDesc rows;      // tgt rows only
@@ -56,39 +62,46 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 __device__ __forceinline__ float order_value(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
-__device__ __forceinline__ uint64_t top_key(float x, int v) {
-  return (static_cast<uint64_t>(order_key(x)) << 32) | static_cast<uint32_t>(~v);
+constexpr uint32_t kOrderNegInf = 0x007fffffu;
+// Largest key first: larger logit, then lower index.
+__device__ __forceinline__ uint64_t top_key(float x, int i) {
+  return (static_cast<uint64_t>(order_key(x)) << 32) | static_cast<uint32_t>(~i);
 }
 
 struct TopLds {
-  uint64_t buf[kTopCap];
+  alignas(16) uint64_t buf[kTopCap + 4];  // (ranking reads four keys at a time)
   uint32_t hist[kThreads];
-  uint32_t maxima[kThreads];
-  uint32_t slot[3];     // candidates appended in a step, three steps' counters in turn
+  uint32_t slot[3];     // keys appended in a step, three steps' counters in turn
   uint32_t wsum[kWaves];
   uint32_t sel_digit, sel_need, sel_count;
-  uint32_t least;       // order of the least key kept
   uint32_t kept;
   uint32_t bad;
   RedLds<1> red;
 };
 
-// Keep the M largest of the n > M keys in s.buf (in any order); every thread
-// receives the order of the least one kept.  Called by the whole workgroup
+// Keep the M largest of the n > M keys in s.buf, in any order, and return how
+// many those are: M, or, unless `exact`, up to M + kTopSlack where keys tie in
+// their high half.  *least receives a bound below which no kept key's high half
+// lies and that M keys reach.  Radix selection over the keys' bytes; SHORT: the
+// high half's two low bytes follow from its sign (bfloat16).  Called by the whole workgroup
 // with the keys visible to it; ends with a barrier.
-__device__ __forceinline__ uint32_t top_select(TopLds& s, int n, int M) {
+template <bool SHORT>
+__device__ __forceinline__ int top_select(TopLds& s, int n, int M, bool exact, uint32_t* least) {
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   uint64_t prefix = 0, mask = 0;
   uint32_t need = static_cast<uint32_t>(M);
-  for (int shift = 56;; shift -= 8) {
+  int shift = 56;
+#pragma unroll 1
+  while (true) {
     s.hist[t] = 0;
     __syncthreads();
+#pragma unroll 1
     for (int i = t; i < n; i += kThreads) {
       const uint64_t k = s.buf[i];
       if ((k & mask) == prefix) atomicAdd(&s.hist[static_cast<int>(k >> shift) & 255], 1u);
     }
     __syncthreads();
-    // keys with a digit above 255 - t
+    // keys with a digit of at least 255 - t
     const uint32_t own = s.hist[255 - t];
     uint32_t inc = own;
 #pragma unroll
@@ -106,78 +119,81 @@ __device__ __forceinline__ uint32_t top_select(TopLds& s, int n, int M) {
       s.sel_need = need - (inc - own);
       s.sel_count = own;
     }
+    if (t == 0) s.kept = 0;
     __syncthreads();
     prefix |= static_cast<uint64_t>(s.sel_digit) << shift;
     mask |= uint64_t{255} << shift;
     need = s.sel_need;
-    if (s.sel_count == need || shift == 0) break;  // all keys of the prefix are kept
+    const uint32_t count = s.sel_count;  // keys of the prefix
+    if (count == need || shift == 0) break;
+    shift -= 8;
+    if (SHORT && shift == 40) {
+      // all zeros, or all ones in the order of a negative number
+      if (!(prefix >> 63)) prefix |= uint64_t{0xffff} << 32;
+      mask |= uint64_t{0xffff} << 32;
+      shift = 24;
+    }
+    if (shift == 24 && !exact && count - need <= static_cast<uint32_t>(kTopSlack)) break;  // ties are kept
   }
-  // move the kept keys to the front
-  constexpr int PER = (kTopCap + kThreads - 1) / kThreads;
+  constexpr int PER = kTopCap / kThreads;
   uint64_t own[PER];
 #pragma unroll
   for (int u = 0; u < PER; ++u) {
     const int i = t + u * kThreads;
     own[u] = i < n ? s.buf[i] : 0;
   }
-  if (t == 0) {
-    s.kept = 0;
-    s.least = 0xffffffffu;
-  }
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    if (t + u * kThreads < n && own[u] >= prefix) {
-      s.buf[atomicAdd(&s.kept, 1u)] = own[u];
-      atomicMin(&s.least, static_cast<uint32_t>(own[u] >> 32));
-    }
-  }
+  for (int u = 0; u < PER; ++u)
+    if (t + u * kThreads < n && own[u] >= prefix) s.buf[atomicAdd(&s.kept, 1u)] = own[u];
   __syncthreads();
-  return s.least;
+  *least = static_cast<uint32_t>(prefix >> 32);
+  return static_cast<int>(s.kept);
 }
 
-// Rank of each of this thread's keys t and t + 256 among the n <= kTopRank
-// keys of s.buf (keys are distinct); rank n for a slot beyond them.
-__device__ __forceinline__ void top_rank(const TopLds& s, int n, uint64_t (&k)[2], int (&rank)[2]) {
+// The n candidates of s.buf sorted, the M largest of them (largest first) in its
+// front; returns how many those are.  Called by the whole workgroup with the keys
+// visible to it; ends with a barrier.  (Keys are distinct, so a key's place is
+// the number of larger ones.)
+template <bool SHORT>
+__device__ __forceinline__ int top_sort(TopLds& s, int n, int M) {
   const int t = threadIdx.x;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int i = t + u * kThreads;
-    k[u] = i < n ? s.buf[i] : 0;
-    rank[u] = i < n ? 0 : n;
-  }
-  if (t >= n) return;
-  for (int j = 0; j < n; ++j) {
-    const uint64_t o = s.buf[j];
-    rank[0] += o > k[0] ? 1 : 0;
-    if (n > kThreads && k[1]) rank[1] += o > k[1] ? 1 : 0;
-  }
-}
-
-// The sorted list of the n candidates in s.buf: row r of the outputs.
-__device__ __forceinline__ void top_write(TopLds& s, int n, const TopArgs& a, int64_t r, bool bad) {
-  const int t = threadIdx.x;
-  int32_t* ids = a.ids + r * a.M;
-  float* values = a.values + r * a.M;
-  const float none = bad ? __builtin_nanf("") : -INFINITY;
-  if (bad) n = 0;
   if (n > kTopRank) {
-    top_select(s, n, a.M);
-    n = a.M;
+    uint32_t least;
+    n = top_select<SHORT>(s, n, M, true, &least);
   }
-  uint64_t k[2];
-  int rank[2];
-  top_rank(s, n, k, rank);
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-    if (t + u * kThreads < n && rank[u] < a.M) {
-      ids[rank[u]] = static_cast<int32_t>(~static_cast<uint32_t>(k[u]));
-      values[rank[u]] = order_value(static_cast<uint32_t>(k[u] >> 32));
+  const uint64_t k0 = t < n ? s.buf[t] : 0, k1 = t + kThreads < n ? s.buf[t + kThreads] : 0;
+  if (t < 4) s.buf[n + t] = 0;
+  __syncthreads();
+  int r0 = 0, r1 = 0;
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+  const u64x2* keys = reinterpret_cast<const u64x2*>(s.buf);
+  if (n > kThreads) {
+#pragma unroll 1
+    for (int j = 0; j < n; j += 4) {
+      const u64x2 a = keys[j >> 1], b = keys[(j >> 1) + 1];
+      r0 += (a.x > k0) + (a.y > k0) + (b.x > k0) + (b.y > k0);
+      r1 += (a.x > k1) + (a.y > k1) + (b.x > k1) + (b.y > k1);
     }
-  if (t >= n && t < a.M) {
-    ids[t] = -1;
-    values[t] = none;
+  } else if ((t & ~63) < n) {
+#pragma unroll 1
+    for (int j = 0; j < n; j += 4) {
+      const u64x2 a = keys[j >> 1], b = keys[(j >> 1) + 1];
+      r0 += (a.x > k0) + (a.y > k0) + (b.x > k0) + (b.y > k0);
+    }
   }
+  __syncthreads();
+  if (k0 && r0 < M) s.buf[r0] = k0;
+  if (k1 && r1 < M) s.buf[r1] = k1;
+  __syncthreads();
+  return n < M ? n : M;
+}
+
+// The lanes of `hit` append their keys to s.buf at base and beyond.
+__device__ __forceinline__ void top_put(TopLds& s, uint64_t hit, uint32_t base, float x, int i) {
+  const uint32_t pos = base + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(hit >> 32),
+                                                        __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(hit), 0));
+  if ((hit >> (threadIdx.x & 63)) & 1) s.buf[pos] = top_key(x, i);
 }
 
 // log sum exp(z / T) from the largest logit and the sum relative to it.
@@ -186,11 +202,42 @@ __device__ __forceinline__ float top_logz(float M, float T, double D) {
                         : static_cast<float>(static_cast<double>(M) / static_cast<double>(T) + log(D));
 }
 
+// The sorted list of n keys in s.buf as row r of the outputs.
+__device__ __forceinline__ void top_write(const TopLds& s, int n, const TopArgs& a, int64_t r, bool bad) {
+  const int t = threadIdx.x;
+  if (t >= a.M) return;
+  const uint64_t k = t < n ? s.buf[t] : 0;
+  a.ids[r * a.M + t] = t < n ? static_cast<int32_t>(~static_cast<uint32_t>(k)) : -1;
+  a.values[r * a.M + t] = t < n ? order_value(static_cast<uint32_t>(k >> 32)) : (bad ? __builtin_nanf("") : -INFINITY);
+}
+
+// sum of exp((x - ref) / T) over one step's logits of a thread, sc = log2(e) / T.
+// One fused multiply-add and one exponential per logit; what the product ref sc
+// loses to rounding is given back to the sum.  References whose product is not
+// finite (rows of the lowest values) take the difference first.
+template <int S, int EPV>
+__device__ __forceinline__ double top_exp_sum(const float (&x)[S][EPV], float ref, float sc) {
+  const float c = ref * sc;
+  float sum = 0.f;
+  if (__any(!(fabsf(c) < INFINITY))) {
+#pragma unroll
+    for (int j = 0; j < S; ++j)
+#pragma unroll
+      for (int k = 0; k < EPV; ++k) sum += __builtin_amdgcn_exp2f((x[j][k] - ref) * sc);
+    return static_cast<double>(sum);
+  }
+#pragma unroll
+  for (int j = 0; j < S; ++j)
+#pragma unroll
+    for (int k = 0; k < EPV; ++k) sum += __builtin_amdgcn_exp2f(fmaf(x[j][k], sc, -c));
+  return static_cast<double>(sum) * (1.0 - kLn2D * static_cast<double>(fmaf(ref, sc, -c)));
+}
+
 // One part of one row.  LZ: the log partition function is asked for.
 template <class E, bool LZ>
-__global__ __launch_bounds__(kThreads) void top_part_kernel(TopArgs a) {
-  constexpr int EPV = E::EPV, S = kTopStep, TILE = kThreads * EPV;
-  static_assert(TILE + kTopMax <= kTopCap, "a selection makes room for a tile");
+__global__ __launch_bounds__(kThreads, kTopWaves) void top_part_kernel(TopArgs a) {
+  constexpr int EPV = E::EPV, S = kTopStep, STEP = kTopStepVecs * EPV;
+  constexpr bool SHORT = sizeof(typename E::raw) == 2;
   __shared__ TopLds s;
   const int t = threadIdx.x;
   const int64_t r = static_cast<int64_t>(blockIdx.x) / a.P;
@@ -201,19 +248,22 @@ __global__ __launch_bounds__(kThreads) void top_part_kernel(TopArgs a) {
   const float sc = temperature_ok(T) ? scale_of(T) : 1.0f;
   const int lo = part * a.part;
   const int hi = a.rows.V - lo < a.part ? a.rows.V : lo + a.part;
+  RawSpan<E, S, kThreads> next;
+  next.issue(row, lo, t, hi);
   if (t < 3) s.slot[t] = 0;
   if (t == 0) s.bad = 0;
   float thr = -INFINITY;
-  bool equal = false;  // logits equal to the threshold are candidates too
-  int n = 0;           // candidates in s.buf
-  float top = -INFINITY, ref = -INFINITY;
+  int n = 0;  // keys in s.buf
+  float top = -INFINITY;
   double D = 0.0;
   __syncthreads();
-  for (int e = lo, step = 0; e < hi; e += S * TILE, ++step) {
+#pragma unroll 1
+  for (int e = lo, step = 0; e < hi; e += STEP, ++step) {
     float x[S][EPV];
-    load_span<E, S, kThreads>(row, e, t, hi, x);
+    next.expand(row, e, t, hi, x);
+    if (hi - e > STEP) next.issue(row, e + STEP, t, hi);  // in flight while this step is worked on
     float vmax[S];
-    float tmax = -INFINITY;
+    float tmax = top;
 #pragma unroll
     for (int j = 0; j < S; ++j) {
       vmax[j] = x[j][0];
@@ -221,98 +271,91 @@ __global__ __launch_bounds__(kThreads) void top_part_kernel(TopArgs a) {
       for (int k = 1; k < EPV; ++k) vmax[j] = max_nan(vmax[j], x[j][k]);
       tmax = max_nan(tmax, vmax[j]);
     }
-    top = max_nan(top, tmax);
-    if (LZ) {
-      const float nr = max_nan(ref, tmax);
-      if (nr != -INFINITY) {
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < S; ++j)
-#pragma unroll
-          for (int k = 0; k < EPV; ++k) sum += __builtin_amdgcn_exp2f((x[j][k] - nr) * sc);
-        if (ref != -INFINITY && nr != ref) D *= static_cast<double>(__builtin_amdgcn_exp2f((ref - nr) * sc));
-        D += static_cast<double>(sum);
-        ref = nr;
-      }
+    if (LZ && tmax != -INFINITY) {
+      if (tmax != top && top != -INFINITY) D *= static_cast<double>(__builtin_amdgcn_exp2f((top - tmax) * sc));
+      D += top_exp_sum(x, tmax, sc);
     }
-    if (step == 0) {
-      // the M-th largest of the threads' maxima, ties by thread
-      const uint32_t mine = order_key(tmax);
-      s.maxima[t] = mine;
-      __syncthreads();
-      int rank = 0;
-      for (int j = 0; j < kThreads; ++j) {
-        const uint32_t o = s.maxima[j];
-        rank += (o > mine || (o == mine && j < t)) ? 1 : 0;
-      }
-      if (rank == a.M - 1) s.least = mine;
-      __syncthreads();
-      thr = order_value(s.least);
-      equal = thr > -INFINITY;
-    }
-    const int at = step % 3;
+    top = tmax;
+    // the step's vectors above the threshold
+    uint64_t hit[S];
+    uint32_t total = 0;
 #pragma unroll
     for (int j = 0; j < S; ++j) {
-      if (vmax[j] > thr || (equal && vmax[j] == thr)) {
-        const int v0 = e + (j * kThreads + t) * EPV;
+      hit[j] = __ballot(vmax[j] > thr);
+      total += __popcll(hit[j]);
+    }
+    const int at = step % 3;
+    if (total) {
+      uint32_t base = 0;
+      if ((t & 63) == 0) base = atomicAdd(&s.slot[at], total);
+      base = n + __builtin_amdgcn_readfirstlane(base);
 #pragma unroll
-        for (int k = 0; k < EPV; ++k)
-          if (x[j][k] > thr || (equal && x[j][k] == thr)) {
-            const uint32_t pos = n + atomicAdd(&s.slot[at], 1u);
-            if (pos < kTopCap) s.buf[pos] = top_key(x[j][k], v0 + k);
-          }
+      for (int j = 0; j < S; ++j) {
+        if (hit[j]) top_put(s, hit[j], base, vmax[j], (e - lo) / EPV + j * kThreads + t);
+        base += __popcll(hit[j]);
       }
     }
     if (t == 0) s.slot[(step + 1) % 3] = 0;
     __syncthreads();
-    const int added = static_cast<int>(s.slot[at]);
-    if (n + added <= kTopCap) {
-      n += added;
-    } else {
-      // again tile by tile, each with room for all of its logits
-      for (int j = 0; j < S; ++j) {
-        if (n > a.M) {
-          thr = order_value(top_select(s, n, a.M));
-          equal = false;
-          n = a.M;
-        }
-        __syncthreads();
-        if (t == 0) s.kept = 0;
-        __syncthreads();
-        const int v0 = e + (j * kThreads + t) * EPV;
-#pragma unroll
-        for (int jj = 0; jj < S; ++jj)
-          if (jj == j) {
-#pragma unroll
-            for (int k = 0; k < EPV; ++k)
-              if (x[jj][k] > thr || (equal && x[jj][k] == thr))
-                s.buf[n + atomicAdd(&s.kept, 1u)] = top_key(x[jj][k], v0 + k);
-          }
-        __syncthreads();
-        n += static_cast<int>(s.kept);
-      }
+    n += static_cast<int>(s.slot[at]);
+    if (n > 2 * a.M + kTopSlack) {
+      uint32_t least;
+      n = top_select<SHORT>(s, n, a.M, false, &least);
+      thr = least > kOrderNegInf ? order_value(least) : -INFINITY;
     }
-    equal = false;
   }
   // a data error: NaN or +inf, a temperature that is none
   if (!(top < INFINITY) || !temperature_ok(T)) atomicOr(&s.bad, 1u);
   float M = 0.f;
   double sum = 0.0;
   if (LZ) {
-    float m[1] = {ref};
+    float m[1] = {top};
     wg_max(m, s.red);  // (ends with a barrier, as wg_sum does)
     M = m[0];
     double d[1] = {0.0};
-    if (ref != -INFINITY) d[0] = D * static_cast<double>(__builtin_amdgcn_exp2f((ref - M) * sc));
+    if (top != -INFINITY) d[0] = D * static_cast<double>(__builtin_amdgcn_exp2f((top - M) * sc));
     wg_sum(d, s.red);
     sum = d[0];
   }
   __syncthreads();
   const bool bad = s.bad != 0;
-  if (a.P == 1) {
-    if (LZ && t == 0) {
-      a.logz[r] = bad ? __builtin_nanf("") : top_logz(M, T, sum);
+  if (bad) n = 0;
+  // the vectors that hold the list, and their logits
+  thr = -INFINITY;
+  if (n > a.M) {
+    uint32_t least;
+    n = top_select<SHORT>(s, n, a.M, true, &least);
+    // (logits equal to the least vector's largest are candidates: one below it)
+    if (least > kOrderNegInf + 1) thr = order_value(least - 1);
+  }
+  const bool mine = t < n;
+  const int v0 = mine ? lo + static_cast<int>(~static_cast<uint32_t>(s.buf[t])) * EPV : lo;
+  float x[1][EPV];
+  load_span<E, 1, 1>(row, v0, 0, hi, x);
+  if (t == 0) s.kept = 0;
+  __syncthreads();
+  uint64_t hit[EPV];
+  uint32_t total = 0;
+#pragma unroll
+  for (int k = 0; k < EPV; ++k) {
+    // order of the zeros: -0 counts as 0
+    hit[k] = __ballot(mine && (x[0][k] > thr || (thr == 0.f && x[0][k] == 0.f)));
+    total += __popcll(hit[k]);
+  }
+  if (total) {
+    uint32_t base = 0;
+    if ((t & 63) == 0) base = atomicAdd(&s.kept, total);
+    base = __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+    for (int k = 0; k < EPV; ++k) {
+      if (hit[k]) top_put(s, hit[k], base, x[0][k], v0 + k);
+      base += __popcll(hit[k]);
     }
+  }
+  __syncthreads();
+  n = top_sort<SHORT>(s, static_cast<int>(s.kept), a.M);
+  if (a.P == 1) {
+    if (LZ && t == 0) a.logz[r] = bad ? __builtin_nanf("") : top_logz(M, T, sum);
     top_write(s, n, a, r, bad);
     return;
   }
@@ -323,19 +366,7 @@ __global__ __launch_bounds__(kThreads) void top_part_kernel(TopArgs a) {
     st.D = bad ? __builtin_nan("") : sum;
     a.stats[r * a.P + part] = st;
   }
-  if (bad) n = 0;
-  if (n > kTopRank) {
-    top_select(s, n, a.M);
-    n = a.M;
-  }
-  uint64_t k[2];
-  int rank[2];
-  top_rank(s, n, k, rank);
-  uint64_t* out = a.cand + (r * a.P + part) * a.M;
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-    if (t + u * kThreads < n && rank[u] < a.M) out[rank[u]] = k[u];
-  if (t >= n && t < a.M) out[t] = 0;
+  if (t < a.M) a.cand[(r * a.P + part) * a.M + t] = t < n ? s.buf[t] : 0;
 }
 
 // The lists of a row's P parts merged.  No key below both bounds can be among
@@ -343,6 +374,8 @@ __global__ __launch_bounds__(kThreads) void top_part_kernel(TopArgs a) {
 // parts' ceil(M / P)-th keys (P ceil(M / P) >= M keys are as large).
 template <bool LZ>
 __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
+  constexpr int PER = 4;  // keys a thread reads at a time
+  static_assert(kTopMax + PER * kThreads <= kTopCap, "a selection makes room for the next keys");
   __shared__ TopLds s;
   __shared__ uint64_t bound[2];
   const int t = threadIdx.x;
@@ -369,22 +402,21 @@ __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
   const bool bad = s.bad != 0;
   const int64_t total = bad ? 0 : static_cast<int64_t>(a.P) * a.M;
   int n = 0;
-  for (int64_t i0 = 0; i0 < total; i0 += 8 * kThreads) {
-    if (n + 8 * kThreads > kTopCap) {
-      // (keys are distinct: one that ties the least kept is that key itself)
-      if (n > a.M) {
-        least = static_cast<uint64_t>(top_select(s, n, a.M)) << 32;
-        n = a.M;
-      }
+#pragma unroll 1
+  for (int64_t i0 = 0; i0 < total; i0 += PER * kThreads) {
+    if (n + PER * kThreads > kTopCap) {
+      uint32_t high;
+      n = top_select<false>(s, n, a.M, true, &high);
+      least = static_cast<uint64_t>(high) << 32;
     }
     __syncthreads();
     if (t == 0) s.kept = 0;
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < PER; ++u) {
       const int64_t i = i0 + u * kThreads + t;
       const uint64_t k = i < total ? cand[i] : 0;
-      if (k >= least) s.buf[n + atomicAdd(&s.kept, 1u)] = k;
+      if (k != 0 && k >= least) s.buf[n + atomicAdd(&s.kept, 1u)] = k;
     }
     __syncthreads();
     n += static_cast<int>(s.kept);
@@ -401,10 +433,9 @@ __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
     for (int p = t; p < a.P; p += 64)
       if (st[p].m != -INFINITY) D += st[p].D * static_cast<double>(__builtin_amdgcn_exp2f((st[p].m - M) * sc));
     D = wave_sum(D);
-    if (t == 0) {
-      a.logz[r] = bad ? __builtin_nanf("") : top_logz(M, T, D);
-    }
+    if (t == 0) a.logz[r] = bad ? __builtin_nanf("") : top_logz(M, T, D);
   }
+  n = top_sort<false>(s, n, a.M);
   top_write(s, n, a, r, bad);
 }
 
