@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kThreads, kTopWaves) void top_part_kernel(TopArgs a
     if (t == 0) s.slot[(step + 1) % 3] = 0;
     __syncthreads();
     n += static_cast<int>(s.slot[at]);
-    if (n > 2 * a.M + kTopSlack) {
+    if (n > 2 * a.M + kTopSlack && hi - e > STEP) {
       uint32_t least;
       n = top_select<SHORT>(s, n, a.M, false, &least);
       thr = least > kOrderNegInf ? order_value(least) : -INFINITY;
@@ -324,7 +324,8 @@ __global__ __launch_bounds__(kThreads, kTopWaves) void top_part_kernel(TopArgs a
   thr = -INFINITY;
   if (n > a.M) {
     uint32_t least;
-    n = top_select<SHORT>(s, n, a.M, true, &least);
+    // (a thread each, and room for all of their logits: ties may stay for short lists)
+    n = top_select<SHORT>(s, n, a.M, a.M + kTopSlack > kThreads, &least);
     // (logits equal to the least vector's largest are candidates: one below it)
     if (least > kOrderNegInf + 1) thr = order_value(least - 1);
   }
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(kThreads, kTopWaves) void top_part_kernel(TopArgs a
 // parts' ceil(M / P)-th keys (P ceil(M / P) >= M keys are as large).
 template <bool LZ>
 __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
-  constexpr int PER = 4;  // keys a thread reads at a time
+  constexpr int PER = 6;  // keys a thread reads at a time
   static_assert(kTopMax + PER * kThreads <= kTopCap, "a selection makes room for the next keys");
   __shared__ TopLds s;
   __shared__ uint64_t bound[2];
@@ -382,58 +383,83 @@ __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
   const int64_t r = blockIdx.x;
   const uint64_t* cand = a.cand + r * a.P * a.M;
   const RowStat* st = a.stats + r * a.P;
+  const int64_t all = static_cast<int64_t>(a.P) * a.M;
+  // every load that depends on no other first
+  uint64_t key[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) key[u] = u * kThreads + t < all ? cand[u * kThreads + t] : 0;
+  const int j0 = (a.M + a.P - 1) / a.P - 1;
+  uint64_t last = 0, among = ~uint64_t{0};
+  RowStat own;
+  own.m = -INFINITY;
+  own.D = 0.0;
+  float top = -INFINITY;
+  bool nan = false;
+  for (int p = t; p < a.P; p += kThreads) {
+    const uint64_t x = cand[static_cast<int64_t>(p) * a.M + a.M - 1], y = cand[static_cast<int64_t>(p) * a.M + j0];
+    const RowStat q = st[p];
+    last = x > last ? x : last;
+    among = y < among ? y : among;
+    top = fmaxf(top, q.m);
+    nan = nan || q.D != q.D;
+    if (p == t) own = q;
+  }
   if (t == 0) {
     s.bad = 0;
+    s.kept = 0;
     bound[0] = 0;
     bound[1] = ~uint64_t{0};
   }
   __syncthreads();
-  const int j0 = (a.M + a.P - 1) / a.P - 1;
-  for (int p = t; p < a.P; p += kThreads) {
-    atomicMax(reinterpret_cast<unsigned long long*>(&bound[0]),
-              static_cast<unsigned long long>(cand[static_cast<int64_t>(p) * a.M + a.M - 1]));
-    atomicMin(reinterpret_cast<unsigned long long*>(&bound[1]),
-              static_cast<unsigned long long>(cand[static_cast<int64_t>(p) * a.M + j0]));
-    if (st[p].D != st[p].D) atomicOr(&s.bad, 1u);
+  if (t < a.P) {
+    atomicMax(reinterpret_cast<unsigned long long*>(&bound[0]), static_cast<unsigned long long>(last));
+    atomicMin(reinterpret_cast<unsigned long long*>(&bound[1]), static_cast<unsigned long long>(among));
+    if (nan) atomicOr(&s.bad, 1u);
   }
   __syncthreads();
   uint64_t least = bound[0] > bound[1] ? bound[0] : bound[1];
   if (least == 0) least = 1;  // empty places
   const bool bad = s.bad != 0;
-  const int64_t total = bad ? 0 : static_cast<int64_t>(a.P) * a.M;
+  const int64_t total = bad ? 0 : all;
   int n = 0;
 #pragma unroll 1
   for (int64_t i0 = 0; i0 < total; i0 += PER * kThreads) {
-    if (n + PER * kThreads > kTopCap) {
-      uint32_t high;
-      n = top_select<false>(s, n, a.M, true, &high);
-      least = static_cast<uint64_t>(high) << 32;
-    }
-    __syncthreads();
-    if (t == 0) s.kept = 0;
-    __syncthreads();
+    if (i0) {
+      if (n + PER * kThreads > kTopCap) {
+        uint32_t high;
+        n = top_select<false>(s, n, a.M, true, &high);
+        least = static_cast<uint64_t>(high) << 32;
+        __syncthreads();
+      }
+      if (t == 0) s.kept = 0;
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t i = i0 + u * kThreads + t;
-      const uint64_t k = i < total ? cand[i] : 0;
-      if (k != 0 && k >= least) s.buf[n + atomicAdd(&s.kept, 1u)] = k;
+      for (int u = 0; u < PER; ++u) {
+        const int64_t i = i0 + u * kThreads + t;
+        key[u] = i < total ? cand[i] : 0;
+      }
+      __syncthreads();
     }
+#pragma unroll
+    for (int u = 0; u < PER; ++u)
+      if (key[u] != 0 && key[u] >= least) s.buf[n + atomicAdd(&s.kept, 1u)] = key[u];
     __syncthreads();
     n += static_cast<int>(s.kept);
+    __syncthreads();
   }
-  if (LZ && t < 64) {
+  if (LZ) {
     int b;
     (void)row_of<BF16>(a.rows, static_cast<int>(r), &b);
     const float T = temperature_of(a.rows, b);
     const float sc = scale_of(T);
-    float M = -INFINITY;
-    for (int p = t; p < a.P; p += 64) M = fmaxf(M, st[p].m);
-    M = wave_max(M);
-    double D = 0.0;
-    for (int p = t; p < a.P; p += 64)
-      if (st[p].m != -INFINITY) D += st[p].D * static_cast<double>(__builtin_amdgcn_exp2f((st[p].m - M) * sc));
-    D = wave_sum(D);
-    if (t == 0) a.logz[r] = bad ? __builtin_nanf("") : top_logz(M, T, D);
+    float m[1] = {top};
+    wg_max(m, s.red);
+    double d[1] = {0.0};
+    for (int p = t; p < a.P; p += kThreads) {
+      const RowStat q = p == t ? own : st[p];
+      if (q.m != -INFINITY) d[0] += q.D * static_cast<double>(__builtin_amdgcn_exp2f((q.m - m[0]) * sc));
+    }
+    wg_sum(d, s.red);
+    if (t == 0) a.logz[r] = bad ? __builtin_nanf("") : top_logz(m[0], T, d[0]);
   }
   n = top_sort<false>(s, n, a.M);
   top_write(s, n, a, r, bad);
