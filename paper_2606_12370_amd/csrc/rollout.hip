@@ -40,8 +40,15 @@ spec_status launched() { return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC
 dim3 groups(int64_t n) { return dim3(static_cast<unsigned>(n)); }
 
 // ---- top logits -------------------------------------------------------------------
-// Workgroups up to which rows are split, each part at least a load step.
-constexpr int64_t kTopGroups = 1024;
+// Workgroups up to which rows are split, each part at least a load step: more of
+// them read a row sooner, and each ends with its own selection and adds a list to
+// the merge.  Measured with up to 256 / 512 / 1024 / 1536 / 2560 workgroups, V =
+// 151936 bfloat16, M = 64, us a call in a graph: R = 16 23.5 / 19.1 / 20.7 / 19.2 /
+// 21.2, R = 64 23.9 / 25.9 / 27.4 / 26.1 / 25.7, R = 96 31.0 / 25.4 / 29.4 / 29.7 /
+// 34.0, R = 192 38.3 / 34.5 / 30.4 / 35.0 / 42.3, R = 384 43.6 / 43.8 / 39.1 / 40.4 /
+// 46.8, R = 768 51.2 / 51.4 / 51.1 / 58.9 / 63.8, R = 1024 63.6 / 63.6 / 63.6 / 63.7 /
+// 77.0; float32 and V = 32000 alike.
+constexpr int64_t kTopGroups = 768;
 
 struct TopPlan {
   int P = 1, part = 0;

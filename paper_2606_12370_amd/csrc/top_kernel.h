@@ -22,6 +22,8 @@
 // split each row over several workgroups, whose lists a second launch merges.
 #pragma once
 
+#include <type_traits>
+
 #include "sv_device.h"
 
 namespace sv {
@@ -79,36 +81,64 @@ struct TopLds {
   RedLds<1> red;
 };
 
+// Inclusive sum over the lanes of a wave: shifts within rows of 16 lanes, then
+// the rows' totals passed on.
+__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v) {
+  const auto from = [](uint32_t x, auto ctrl, auto rows) {
+    return static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  using std::integral_constant;
+  v += from(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // row_shr 1
+  v += from(v, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  v += from(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  v += from(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  v += from(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // lane 15 to row 1, lane 47 to row 3
+  v += from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // lane 31 to rows 2 and 3
+  return v;
+}
+
 // Keep the M largest of the n > M keys in s.buf, in any order, and return how
 // many those are: M, or, unless `exact`, up to M + kTopSlack where keys tie in
 // their high half.  *least receives a bound below which no kept key's high half
 // lies and that M keys reach.  Radix selection over the keys' bytes; SHORT: the
-// high half's two low bytes follow from its sign (bfloat16).  Called by the whole workgroup
-// with the keys visible to it; ends with a barrier.
-template <bool SHORT>
+// high half's two low bytes follow from its sign (bfloat16).  HELD: the thread's keys stay in
+// registers, one LDS latency instead of one a byte; not within a pass over a row,
+// whose loads in flight need the registers (12288 rows, M = 1: 580 us a call
+// with keys read again, 650 held).  Called by the whole workgroup with the keys
+// visible to it; ends with a barrier.
+template <bool SHORT, bool HELD = true>
 __device__ __forceinline__ int top_select(TopLds& s, int n, int M, bool exact, uint32_t* least) {
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   uint64_t prefix = 0, mask = 0;
   uint32_t need = static_cast<uint32_t>(M);
   int shift = 56;
+  constexpr int PER = kTopCap / kThreads;
+  uint64_t key[HELD ? PER : 1];
+  if constexpr (HELD) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) key[u] = t + u * kThreads < n ? s.buf[t + u * kThreads] : 0;
+  }
 #pragma unroll 1
   while (true) {
     s.hist[t] = 0;
     __syncthreads();
+    if constexpr (HELD) {
+#pragma unroll
+      for (int u = 0; u < PER; ++u)
+        if (u * kThreads < n && t + u * kThreads < n && (key[u] & mask) == prefix)
+          atomicAdd(&s.hist[static_cast<int>(key[u] >> shift) & 255], 1u);
+    } else {
 #pragma unroll 1
-    for (int i = t; i < n; i += kThreads) {
-      const uint64_t k = s.buf[i];
-      if ((k & mask) == prefix) atomicAdd(&s.hist[static_cast<int>(k >> shift) & 255], 1u);
+      for (int i = t; i < n; i += kThreads) {
+        const uint64_t k = s.buf[i];
+        if ((k & mask) == prefix) atomicAdd(&s.hist[static_cast<int>(k >> shift) & 255], 1u);
+      }
     }
     __syncthreads();
     // keys with a digit of at least 255 - t
     const uint32_t own = s.hist[255 - t];
-    uint32_t inc = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t up = __shfl_up(inc, o, 64);
-      if (lane >= o) inc += up;
-    }
+    uint32_t inc = wave_scan_u32(own);
     if (lane == 63) s.wsum[wave] = inc;
     __syncthreads();
 #pragma unroll
@@ -135,18 +165,21 @@ __device__ __forceinline__ int top_select(TopLds& s, int n, int M, bool exact, u
     }
     if (shift == 24 && !exact && count - need <= static_cast<uint32_t>(kTopSlack)) break;  // ties are kept
   }
-  constexpr int PER = kTopCap / kThreads;
-  uint64_t own[PER];
+  if constexpr (HELD) {
 #pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    const int i = t + u * kThreads;
-    own[u] = i < n ? s.buf[i] : 0;
+    for (int u = 0; u < PER; ++u)
+      if (u * kThreads < n && t + u * kThreads < n && key[u] >= prefix) s.buf[atomicAdd(&s.kept, 1u)] = key[u];
+    __syncthreads();
+  } else {
+    // 256 keys at a time: the places filled so far lie before the keys still to be read
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+      const uint64_t k = i0 + t < n ? s.buf[i0 + t] : 0;
+      __syncthreads();
+      if (i0 + t < n && k >= prefix) s.buf[atomicAdd(&s.kept, 1u)] = k;
+      __syncthreads();
+    }
   }
-  __syncthreads();
-#pragma unroll
-  for (int u = 0; u < PER; ++u)
-    if (t + u * kThreads < n && own[u] >= prefix) s.buf[atomicAdd(&s.kept, 1u)] = own[u];
-  __syncthreads();
   *least = static_cast<uint32_t>(prefix >> 32);
   return static_cast<int>(s.kept);
 }
@@ -169,14 +202,14 @@ __device__ __forceinline__ int top_sort(TopLds& s, int n, int M) {
   typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
   const u64x2* keys = reinterpret_cast<const u64x2*>(s.buf);
   if (n > kThreads) {
-#pragma unroll 1
+#pragma unroll 4
     for (int j = 0; j < n; j += 4) {
       const u64x2 a = keys[j >> 1], b = keys[(j >> 1) + 1];
       r0 += (a.x > k0) + (a.y > k0) + (b.x > k0) + (b.y > k0);
       r1 += (a.x > k1) + (a.y > k1) + (b.x > k1) + (b.y > k1);
     }
   } else if ((t & ~63) < n) {
-#pragma unroll 1
+#pragma unroll 4
     for (int j = 0; j < n; j += 4) {
       const u64x2 a = keys[j >> 1], b = keys[(j >> 1) + 1];
       r0 += (a.x > k0) + (a.y > k0) + (b.x > k0) + (b.y > k0);
@@ -300,7 +333,7 @@ __global__ __launch_bounds__(kThreads, kTopWaves) void top_part_kernel(TopArgs a
     n += static_cast<int>(s.slot[at]);
     if (n > 2 * a.M + kTopSlack && hi - e > STEP) {
       uint32_t least;
-      n = top_select<SHORT>(s, n, a.M, false, &least);
+      n = top_select<SHORT, false>(s, n, a.M, false, &least);
       thr = least > kOrderNegInf ? order_value(least) : -INFINITY;
     }
   }
@@ -393,14 +426,12 @@ __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
   RowStat own;
   own.m = -INFINITY;
   own.D = 0.0;
-  float top = -INFINITY;
   bool nan = false;
   for (int p = t; p < a.P; p += kThreads) {
     const uint64_t x = cand[static_cast<int64_t>(p) * a.M + a.M - 1], y = cand[static_cast<int64_t>(p) * a.M + j0];
     const RowStat q = st[p];
     last = x > last ? x : last;
     among = y < among ? y : among;
-    top = fmaxf(top, q.m);
     nan = nan || q.D != q.D;
     if (p == t) own = q;
   }
@@ -446,20 +477,21 @@ __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
     n += static_cast<int>(s.kept);
     __syncthreads();
   }
-  if (LZ) {
+  if (LZ && t < 64) {
     int b;
     (void)row_of<BF16>(a.rows, static_cast<int>(r), &b);
     const float T = temperature_of(a.rows, b);
     const float sc = scale_of(T);
-    float m[1] = {top};
-    wg_max(m, s.red);
-    double d[1] = {0.0};
-    for (int p = t; p < a.P; p += kThreads) {
-      const RowStat q = p == t ? own : st[p];
-      if (q.m != -INFINITY) d[0] += q.D * static_cast<double>(__builtin_amdgcn_exp2f((q.m - m[0]) * sc));
+    float m = -INFINITY;
+    for (int p = t; p < a.P; p += 64) m = fmaxf(m, p == t ? own.m : st[p].m);
+    m = wave_max(m);
+    double d = 0.0;
+    for (int p = t; p < a.P; p += 64) {
+      const float mp = p == t ? own.m : st[p].m;
+      if (mp != -INFINITY) d += (p == t ? own.D : st[p].D) * static_cast<double>(__builtin_amdgcn_exp2f((mp - m) * sc));
     }
-    wg_sum(d, s.red);
-    if (t == 0) a.logz[r] = bad ? __builtin_nanf("") : top_logz(m[0], T, d[0]);
+    d = wave_sum(d);
+    if (t == 0) a.logz[r] = bad ? __builtin_nanf("") : top_logz(m, T, d);
   }
   n = top_sort<false>(s, n, a.M);
   top_write(s, n, a, r, bad);
