@@ -20,10 +20,15 @@
 // exponentials of the row float32, their sums float32 over at most 128 elements
 // and float64 beyond.
 //
-// Launches: 1 distill_stats (a wave per list, and a wave per sub-chunk of the
-// student's row), 2 distill_grad (a workgroup per chunk), or distill_norm
-// without a gradient, 3 distill_loss.
+// Launches, with a gradient of many rows that fit the registers: 1 distill_lists
+// (a wave per list), 2 distill_row (workgroups that hold whole rows), 3
+// distill_close (the listed tokens), 4 distill_loss.  Otherwise: 1 distill_stats
+// (a wave per list, and a wave per sub-chunk of the student's row), 2
+// distill_grad (a workgroup per chunk), or distill_norm without a gradient, 3
+// distill_loss.
 #pragma once
+
+#include <type_traits>
 
 #include "sv_device.h"
 
@@ -48,12 +53,12 @@ struct ListInfo {
   double Dl;     // sum of exp((z - ml) / T) over the listed tokens (with a teacher log Z, else 0)
   float ml;      // the largest listed logit of the student (-inf: none)
   int state;     // 0: an empty list, 1: ordinary, 2: a data error
+  int again;     // an id is listed more than once
+  int pad;
 };
 
 // A row's normalisers.
 struct DistillNorm {
-  double logD;   // log sum exp(z / T) - M / T
-  double logDo;  // log of the unlisted sum, - M / T too
   double D;      // sum relative to M
   double Do;     // unlisted sum relative to mo
   float M, mo;   // the row's largest logit and the largest unlisted one (mo = M without a teacher log Z)
@@ -74,6 +79,11 @@ struct DistillArgs {
   ListInfo* info;         // [N K]
   DistillStat* stats;     // [N K][C]
   double* part;           // [N K] per-step losses
+  // distill_row: rows with a list, then the others; how many the former are, and the
+  // next row that no workgroup has taken
+  int32_t* order;         // [N K]
+  int32_t* states;        // [N K], of ListInfo
+  uint32_t* head;         // [2]
 };
 
 // exp((z - ref) / T) for z <= ref.  The difference comes first, so that a row
@@ -83,6 +93,13 @@ struct DistillArgs {
 __device__ __forceinline__ float scaled_exp(float z, float s_hi, float s_lo, float ref) {
   const float d = z - ref;
   return __builtin_amdgcn_exp2f(fmaf(d, s_hi, d * s_lo));
+}
+
+// exp(d / T) for d <= 0 to float32's precision, in float64's range.
+__device__ __forceinline__ double exp_of(double d, double inv_t) {
+  const double x = fmax(d * inv_t * kLog2eD, -2000.0);
+  const double n = rint(x);
+  return ldexp(static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(x - n))), static_cast<int>(n));
 }
 
 __device__ __forceinline__ void unit_of(const DistillArgs& a, int64_t u, int* n, int* k) {
@@ -101,14 +118,13 @@ __device__ __forceinline__ double wave_max_d(double v) {
   return v;
 }
 
-// The teacher's side of one position, by one wave (64 entries at a time).
-template <class E>
-__device__ __forceinline__ ListInfo list_info(const DistillArgs& a, int n, int k) {
+// The teacher's side of one position, by one wave of PER entries a lane.
+template <class E, int PER>
+__device__ __forceinline__ ListInfo list_info_of(const DistillArgs& a, int n, int k) {
   const int lane = threadIdx.x & 63;
   const int32_t* ids = a.ids + list_of(a, n, k);
   const float* vals = a.vals + list_of(a, n, k);
   const typename E::raw* row = student_row<E>(a, n, k);
-  constexpr int PER = kListMax / 64;
   int id[PER];
   double t[PER], z[PER];
   bool used = false, bad = false;
@@ -180,39 +196,52 @@ __device__ __forceinline__ ListInfo list_info(const DistillArgs& a, int n, int k
     }
   }
   o.state = bad ? 2 : (any ? 1 : 0);
+  // an entry with the id of an earlier one
+  bool again[PER] = {};
+  for (int j = 0; j < a.M; ++j) {
+    int other = id[0];
+#pragma unroll
+    for (int u = 1; u < PER; ++u) other = (j >> 6) == u ? id[u] : other;
+    other = __builtin_amdgcn_readlane(other, j & 63);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) again[u] = again[u] || (other == id[u] && other >= 0 && j < u * 64 + lane);
+  }
+  bool twice = false;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) twice = twice || again[u];
+  o.again = __ballot(twice) != 0 ? 1 : 0;
+  o.pad = 0;
   o.Dl = 0.0;
   if (a.logz) {
-    // each listed token once: an entry with the id of an earlier one is left out
-    bool again[PER] = {};
-    for (int j = 0; j < a.M; ++j) {
-      int other = id[0];
-#pragma unroll
-      for (int u = 1; u < PER; ++u) other = (j >> 6) == u ? id[u] : other;
-      other = __builtin_amdgcn_readlane(other, j & 63);
-#pragma unroll
-      for (int u = 0; u < PER; ++u) again[u] = again[u] || (other == id[u] && j < u * 64 + lane);
-    }
     double d = 0.0;
 #pragma unroll
     for (int u = 0; u < PER; ++u)
-      if (!again[u] && z[u] > -INFINITY) d += exp(z[u]);
+      if (id[u] >= 0 && !again[u] && z[u] > -INFINITY) d += exp(z[u]);
     o.Dl = wave_sum(d);
   }
   return o;
 }
+template <class E>
+__device__ __forceinline__ ListInfo list_info(const DistillArgs& a, int n, int k) {
+  if (a.M <= 64) return list_info_of<E, 1>(a, n, k);
+  if (a.M <= 128) return list_info_of<E, 2>(a, n, k);
+  return list_info_of<E, kListMax / 64>(a, n, k);
+}
 
-// A row's normalisers from its sub-chunks' sums (m, D) and its list.
+// A row's normalisers from its sums (m, D) and its list; without TAIL the sums
+// hold the whole row.
+template <bool TAIL>
 __device__ __forceinline__ DistillNorm distill_norm(const DistillArgs& a, const ListInfo& li, float m, double D) {
   DistillNorm n;
   n.mo = m;
   n.Do = D;
+  n.M = m;
+  n.D = D;
+  if (!TAIL) return n;
   n.M = fmaxf(m, li.ml);
-  const double wo = m == -INFINITY ? 0.0 : exp((static_cast<double>(m) - static_cast<double>(n.M)) * a.inv_t);
-  const double wl = li.Dl > 0.0 ? exp((static_cast<double>(li.ml) - static_cast<double>(n.M)) * a.inv_t) : 0.0;
+  const double wo = m == -INFINITY ? 0.0 : exp_of(static_cast<double>(m) - static_cast<double>(n.M), a.inv_t);
+  const double wl = li.Dl > 0.0 ? exp_of(static_cast<double>(li.ml) - static_cast<double>(n.M), a.inv_t) : 0.0;
   n.D = (D != D ? D : D * wo) + li.Dl * wl;
-  n.logD = log(n.D);
-  n.logDo = m == -INFINITY ? -INFINITY
-                           : log(D) + (static_cast<double>(m) - static_cast<double>(n.M)) * a.inv_t;
   return n;
 }
 __device__ __forceinline__ bool norm_ok(const DistillNorm& n) { return n.D > 0.0 && n.D < INFINITY && n.M < INFINITY; }
@@ -222,8 +251,14 @@ __device__ __forceinline__ double distill_loss_of(const DistillArgs& a, const Li
   if (li.state == 0) return 0.0;
   if (li.state == 2 || !norm_ok(n)) return __builtin_nan("");
   const double ref = li.ml > -INFINITY ? static_cast<double>(li.ml) : 0.0;
-  double L = li.c + li.W * ((static_cast<double>(n.M) - ref) * a.inv_t + n.logD);
-  if (li.r > 0.0) L += li.r * (n.logD - n.logDo);
+  const double logD = log(n.D);
+  double L = li.c + li.W * ((static_cast<double>(n.M) - ref) * a.inv_t + logD);
+  if (li.r > 0.0) {
+    const double out = n.mo == -INFINITY
+                           ? -INFINITY
+                           : log(n.Do) + (static_cast<double>(n.mo) - static_cast<double>(n.M)) * a.inv_t;
+    L += li.r * (logD - out);
+  }
   return L;
 }
 
@@ -245,27 +280,7 @@ __device__ __forceinline__ DistillNorm combine_distill(const DistillArgs& a, con
     }
     d = wave_sum(d);
   }
-  return distill_norm(a, li, m, d);
-}
-
-// The entries of a list whose ids lie in [lo, hi), in list order, by one wave:
-// ids into `out` (LDS of the wave, kListMax places; nullptr: none wanted) and
-// their count, -1 for a list without entries.
-__device__ __forceinline__ int list_in_range(const DistillArgs& a, int64_t at, int lo, int hi, int* out) {
-  const int lane = threadIdx.x & 63;
-  int cnt = 0;
-  bool used = false;
-  for (int base = 0; base < a.M; base += 64) {
-    const int j = base + lane;
-    const int id = j < a.M ? a.ids[at + j] : -1;
-    used = used || __ballot(id >= 0) != 0;
-    if (!out) continue;
-    const bool in = id >= lo && id < hi;
-    const uint64_t m = __ballot(in);
-    if (in) out[cnt + __popcll(m & ((uint64_t{1} << lane) - 1))] = id;
-    cnt += __popcll(m);
-  }
-  return used ? cnt : -1;
+  return distill_norm<true>(a, li, m, d);
 }
 
 constexpr int kDistillVec = 16;  // vectors per lane of a sub-chunk
@@ -277,7 +292,8 @@ constexpr int distill_sub() { return kDistillVec * 64 * E::EPV; }
 template <class E, bool TAIL>
 __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, int lists, int64_t nsub) {
   constexpr int EPV = E::EPV, S = 4, W = 64 * EPV, SUB = distill_sub<E>();
-  __shared__ int in_list[TAIL ? kWaves : 1][TAIL ? kListMax : 1];
+  // a bit for every listed logit of a wave's sub-chunk
+  __shared__ uint32_t listed[TAIL ? kWaves : 1][TAIL ? SUB / 32 : 1];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   int n, k;
   if (static_cast<int>(blockIdx.x) < lists) {
@@ -295,13 +311,26 @@ __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, 
   unit_of(a, u, &n, &k);
   const typename E::raw* row = student_row<E>(a, n, k);
   const int e0 = c * SUB;
-  uint32_t tiles = 0;  // tiles of vectors that hold a listed token
-  const int cnt = list_in_range(a, list_of(a, n, k), e0, a.V - e0 < SUB ? a.V : e0 + SUB, TAIL ? in_list[wave] : nullptr);
-  if (cnt < 0) return;  // (nothing reads the statistics of an empty list)
+  uint32_t tiles = 0;  // vectors of the wave that hold a listed token
+  const int32_t* ids = a.ids + list_of(a, n, k);
+  if (TAIL) {
+    for (int i = lane; i < SUB / 32; i += 64) listed[wave][i] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  bool used = false;
+  for (int j = lane; j < a.M; j += 64) {
+    const int o = ids[j];
+    used = used || o >= 0;
+    if (TAIL && o >= e0 && o - e0 < SUB && o < a.V) {
+      atomicOr(&listed[wave][(o - e0) >> 5], 1u << (o & 31));
+      tiles |= 1u << ((o - e0) / W);
+    }
+  }
+  if (__ballot(used) == 0) return;  // (nothing reads the statistics of an empty list)
   if (TAIL) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    for (int j = lane; j < cnt; j += 64) tiles |= 1u << ((in_list[wave][j] - e0) / W);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) tiles |= __shfl_xor(tiles, o, 64);
     tiles = __builtin_amdgcn_readfirstlane(tiles);
@@ -318,13 +347,11 @@ __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, 
 #pragma unroll
       for (int j = 0; j < S; ++j) {
         if ((tiles >> (st * S + j)) & 1u) {
-          const int v0 = es + j * W + lane * EPV;
-          for (int q = 0; q < cnt; ++q) {
-            const int o = in_list[wave][q] - v0;
+          const int o = ((st * S + j) * 64 + lane) * EPV;
+          const uint32_t hit = listed[wave][o >> 5] >> (o & 31);
 #pragma unroll
-            for (int i = 0; i < EPV; ++i)
-              if (o == i) x[j][i] = -INFINITY;
-          }
+          for (int i = 0; i < EPV; ++i)
+            if ((hit >> i) & 1u) x[j][i] = -INFINITY;
         }
       }
     }
@@ -357,6 +384,78 @@ __global__ __launch_bounds__(kThreads) void distill_stats_kernel(DistillArgs a, 
   }
 }
 
+// The lists alone.
+template <class E>
+__global__ __launch_bounds__(kThreads) void distill_lists_kernel(DistillArgs a) {
+  const int64_t u = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  if (u >= static_cast<int64_t>(a.N) * a.K) return;
+  int n, k;
+  unit_of(a, u, &n, &k);
+  const ListInfo li = list_info<E>(a, n, k);
+  if ((threadIdx.x & 63) == 0) {
+    a.info[u] = li;
+    a.states[u] = li.state;
+  }
+}
+
+// The rows in the order in which distill_row takes them: those with a list first
+// (one workgroup; each thread sorts a run of consecutive rows).
+constexpr int kOrderThreads = 1024;
+__global__ __launch_bounds__(kOrderThreads) void distill_order_kernel(DistillArgs a, uint32_t first_ticket) {
+  __shared__ int wsum[kOrderThreads / 64];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int64_t units = static_cast<int64_t>(a.N) * a.K;
+  // runs of whole vectors of four states
+  const int64_t run = (units + 4 * kOrderThreads - 1) / (4 * kOrderThreads) * 4;
+  const int64_t lo = t * run < units ? t * run : units, hi = lo + run < units ? lo + run : units;
+  const auto states = [&](int64_t u, int (&st)[4]) {
+    if (u + 4 <= units) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(a.states + u);
+      st[0] = static_cast<int>(v.x); st[1] = static_cast<int>(v.y);
+      st[2] = static_cast<int>(v.z); st[3] = static_cast<int>(v.w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st[i] = u + i < units ? a.states[u + i] : 0;
+    }
+  };
+  int live = 0;
+#pragma unroll 4
+  for (int64_t u = lo; u < hi; u += 4) {
+    int st[4];
+    states(u, st);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) live += st[i] == 1 ? 1 : 0;
+  }
+  int inc = live;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 63) wsum[wave] = inc;
+  __syncthreads();
+  int before = inc - live, total = 0;
+  for (int w = 0; w < kOrderThreads / 64; ++w) {
+    if (w < wave) before += wsum[w];
+    total += wsum[w];
+  }
+  int64_t at = before, rest = total + lo - before;
+#pragma unroll 4
+  for (int64_t u = lo; u < hi; u += 4) {
+    int st[4];
+    states(u, st);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t place = st[i] == 1 ? at++ : rest++;
+      if (u + i < hi) a.order[place] = static_cast<int32_t>(u + i);
+    }
+  }
+  if (t == 0) {
+    a.head[0] = static_cast<uint32_t>(total);
+    a.head[1] = first_ticket;
+  }
+}
+
 // The loss of every position without a gradient (one wave each).
 __global__ __launch_bounds__(kThreads) void distill_norm_kernel(DistillArgs a) {
   const int64_t u = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
@@ -370,13 +469,19 @@ __global__ __launch_bounds__(kThreads) void distill_norm_kernel(DistillArgs a) {
   }
 }
 
-// Gradient elements: float32, or bfloat16 rounded to nearest even.
+// Gradient elements: float32, or bfloat16 rounded to nearest even.  NT: stored
+// non-temporally, by the launches that read each logit once (N = 4096, K = 3, V =
+// 151936: 2.60 ms a call without, 2.41 with); not by the others, whose second read
+// then finds less of the row in the caches (N = 300, K = 2, V = 100003 float32, the
+// gradient pass 83 us without, 104 with).
 struct GradF32 {
   using raw = float;
+  template <bool NT>
   static __device__ __forceinline__ void store4(raw* p, const float (&g)[4]) {
     f32x4 v;
     v.x = g[0]; v.y = g[1]; v.z = g[2]; v.w = g[3];
-    *reinterpret_cast<f32x4_any*>(p) = v;
+    if (NT) __builtin_nontemporal_store(v, reinterpret_cast<f32x4_any*>(p));
+    else *reinterpret_cast<f32x4_any*>(p) = v;
   }
   static __device__ __forceinline__ void store1(raw* p, float g) { *p = g; }
 };
@@ -388,11 +493,13 @@ struct GradBF16 {
     const f32x2 f = {lo, hi};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
   }
+  template <bool NT>
   static __device__ __forceinline__ void store4(raw* p, const float (&g)[4]) {
     u32x2 v;
     v.x = round2(g[0], g[1]);
     v.y = round2(g[2], g[3]);
-    *reinterpret_cast<u32x2_any*>(p) = v;
+    if (NT) __builtin_nontemporal_store(v, reinterpret_cast<u32x2_any*>(p));
+    else *reinterpret_cast<u32x2_any*>(p) = v;
   }
   static __device__ __forceinline__ void store1(raw* p, float g) { *p = static_cast<uint16_t>(round2(g, 0.f)); }
 };
@@ -403,6 +510,7 @@ struct DistillCoef {
   float cl, cu, ru;
   bool nan;
 };
+template <bool TAIL>
 __device__ __forceinline__ DistillCoef distill_coef(const DistillArgs& a, const ListInfo& li, const DistillNorm& n) {
   DistillCoef c;
   c.nan = li.state == 2 || (li.state == 1 && !norm_ok(n));
@@ -411,72 +519,60 @@ __device__ __forceinline__ DistillCoef distill_coef(const DistillArgs& a, const 
   // where no unlisted token has mass, none has a gradient either
   c.cu = 0.f;
   c.ru = n.mo > -INFINITY ? n.mo : 0.f;
-  if (n.mo > -INFINITY) {
-    const double w = exp((static_cast<double>(n.mo) - static_cast<double>(n.M)) * a.inv_t);
+  if (!TAIL) {
+    c.cu = c.cl;
+  } else if (n.mo > -INFINITY) {
+    const double w = exp_of(static_cast<double>(n.mo) - static_cast<double>(n.M), a.inv_t);
     c.cu = static_cast<float>(all * w - (li.r > 0.0 ? a.f * li.r / n.Do : 0.0));
   }
   return c;
+}
+
+// p_j of an entry, to float32's precision (a list's log Z may lie below its
+// values: no bound on the exponent's sign).
+__device__ __forceinline__ double list_prob(const DistillArgs& a, const ListInfo& li, float value) {
+  const double x = fmin(fmax((static_cast<double>(value) * a.inv_t - li.lse) * kLog2eD, -2000.0), 2000.0);
+  const double w = rint(x);
+  return ldexp(static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(x - w))), static_cast<int>(w));
 }
 
 constexpr int kDistillChunk = 16384;
 
 // One chunk of one row's gradient; the workgroup of chunk 0 also writes the
 // position's loss.  E reads four elements per lane (one 16-byte store each).
+// Every token gets the unlisted tokens' gradient first; thread t then writes that
+// of list entry t, if its token lies in the chunk, over it: behind a wait for the
+// first store's completion and a barrier.  (A search of the list in every vector
+// that may hold a listed token took longer than the chunk where many ids lie
+// close together: N = 8, V = 8000, M = 64 106 us a call.)
 template <class E, class G>
 __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a, int CH) {
   static_assert(E::EPV == 4, "one gradient vector per lane");
+  static_assert(kListMax <= kThreads, "a thread per list entry");
   constexpr int S = 4, TILE = kThreads * 4, NT = kDistillChunk / TILE;
-  __shared__ int in_list[kListMax];
-  __shared__ float in_p[kListMax];
-  __shared__ int count;
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int t = threadIdx.x;
   const int64_t u = static_cast<int64_t>(blockIdx.x) / CH;
   const int c = static_cast<int>(static_cast<int64_t>(blockIdx.x) - u * CH);
   int n, k;
   unit_of(a, u, &n, &k);
   const ListInfo li = a.info[u];
+  const int64_t at = list_of(a, n, k);
+  const typename E::raw* row = student_row<E>(a, n, k);
+  const int e0 = c * kDistillChunk;
+  const int e1 = a.V - e0 < kDistillChunk ? a.V : e0 + kDistillChunk;
+  const int id = t < a.M ? a.ids[at + t] : -1;
+  const bool mine = li.state == 1 && id >= e0 && id < e1;
+  const float z = mine ? E::one(row + id) : 0.f;
+  const float value = mine ? a.vals[at + t] : 0.f;
   const DistillNorm nm = combine_distill(a, li, u);
-  const DistillCoef co = distill_coef(a, li, nm);
+  const DistillCoef co = distill_coef<true>(a, li, nm);
   if (c == 0 && t == 0) {
     const double L = distill_loss_of(a, li, nm);
     a.part[u] = L;
     if (a.per_step) a.per_step[u] = static_cast<float>(L);
   }
-  const int e0 = c * kDistillChunk;
-  const int e1 = a.V - e0 < kDistillChunk ? a.V : e0 + kDistillChunk;
   typename G::raw* out = static_cast<typename G::raw*>(a.grad) + u * a.V;
   const bool plain = li.state == 1 && !co.nan;
-  if (wave == 0) {
-    int cnt = 0;
-    if (plain) {
-      const int64_t at = list_of(a, n, k);
-      for (int base = 0; base < a.M; base += 64) {
-        const int j = base + lane;
-        const int id = j < a.M ? a.ids[at + j] : -1;
-        const bool in = id >= e0 && id < e1;
-        const uint64_t m = __ballot(in);
-        if (in) {
-          const int pos = cnt + __popcll(m & ((uint64_t{1} << lane) - 1));
-          in_list[pos] = id;
-          in_p[pos] = static_cast<float>(a.f * exp(static_cast<double>(a.vals[at + j]) * a.inv_t - li.lse));
-        }
-        cnt += __popcll(m);
-      }
-    }
-    if (lane == 0) count = cnt;
-  }
-  __syncthreads();
-  const int cnt = count;
-  // tiles of this wave that hold a listed token
-  uint32_t tiles = 0;
-  for (int j = lane; j < cnt; j += 64) {
-    const int o = in_list[j] - e0;
-    if ((o % TILE) / 256 == wave) tiles |= 1u << (o / TILE);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) tiles |= __shfl_xor(tiles, o, 64);
-  tiles = __builtin_amdgcn_readfirstlane(tiles);
-  const typename E::raw* row = student_row<E>(a, n, k);
   const float fill = co.nan ? __builtin_nanf("") : 0.f;
 #pragma unroll 1
   for (int st = 0; st < NT / S; ++st) {
@@ -487,32 +583,13 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a, i
 #pragma unroll
     for (int j = 0; j < S; ++j) {
       const int v0 = es + (j * kThreads + t) * 4;
-      float g[4];
+      float g[4] = {fill, fill, fill, fill};
       if (plain) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) g[i] = co.cu * scaled_exp(x[j][i], a.s_hi, a.s_lo, co.ru);
-        if ((tiles >> (st * S + j)) & 1u) {
-          float p[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t hit = 0;
-          for (int q = 0; q < cnt; ++q) {
-            const int o = in_list[q] - v0;
-            if (o >= 0 && o < 4) {
-              hit |= 1u << o;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (i == o) p[i] += in_p[q];
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if ((hit >> i) & 1u) g[i] = co.cl * scaled_exp(x[j][i], a.s_hi, a.s_lo, nm.M) - p[i];
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = fill;
       }
       if (v0 + 4 <= a.V) {
-        G::store4(out + v0, g);
+        G::template store4<false>(out + v0, g);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -520,16 +597,379 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a, i
       }
     }
   }
+  if (!plain) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (mine) {
+    double p = list_prob(a, li, value);
+    if (li.again) {
+      p = 0.0;
+      for (int j = 0; j < a.M; ++j)
+        if (a.ids[at + j] == id) p += list_prob(a, li, a.vals[at + j]);
+    }
+    G::store1(out + id, co.cl * scaled_exp(z, a.s_hi, a.s_lo, nm.M) - static_cast<float>(a.f * p));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows held in registers.  A workgroup of TH threads takes whole rows: a row is
+// loaded once, into NV vectors of four logits a thread; its sums are formed from
+// the registers; its gradient is written from them, and the next row's loads of a
+// vector are issued as soon as the vector is free, so that reads and writes
+// overlap although the workgroup has its CU (or half of it) for itself.  Rows are
+// handed out as workgroups come for them, those without a list last.
+//
+// Every token gets the unlisted tokens' gradient here; distill_close_kernel
+// writes the listed ones' over it, a launch later.  With a teacher log Z (TAIL)
+// the listed logits are left out of the sums: their places are bits in LDS, one
+// per logit of a thread, beside a mask of the tiles of each wave that hold any.
+template <class E> struct RowVec;
+template <> struct RowVec<BF16H> {
+  // elements moved down by n (0 to 4), -inf from the top
+  static __device__ __forceinline__ u32x2 shift(u32x2 w, int n) {
+    const uint64_t ninf = 0xFF80FF80FF80FF80ull;
+    uint64_t v = (static_cast<uint64_t>(w.y) << 32) | w.x;
+    v = n == 0 ? v : (n >= 4 ? ninf : (v >> (16 * n)) | (ninf << (64 - 16 * n)));
+    return u32x2{static_cast<uint32_t>(v), static_cast<uint32_t>(v >> 32)};
+  }
+  // opaque to the compiler, so that widened logits are formed again behind it
+  // instead of being kept
+  static __device__ __forceinline__ void hide(u32x2& w) { asm volatile("" : "+v"(w)); }
+};
+template <> struct RowVec<F32> {
+  static __device__ __forceinline__ u32x4 shift(u32x4 w, int n) {
+    const uint32_t ninf = 0xFF800000u;
+    u32x4 o;
+    o.x = n == 0 ? w.x : (n == 1 ? w.y : (n == 2 ? w.z : (n == 3 ? w.w : ninf)));
+    o.y = n == 0 ? w.y : (n == 1 ? w.z : (n == 2 ? w.w : ninf));
+    o.z = n == 0 ? w.z : (n == 1 ? w.w : ninf);
+    o.w = n == 0 ? w.w : ninf;
+    return o;
+  }
+  static __device__ __forceinline__ void hide(u32x4& w) { asm volatile("" : "+v"(w)); }
+};
+
+// The same for a scalar: the conditions of a pass over the slots are formed in it.
+__device__ __forceinline__ int opaque_scalar(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
+template <int TH, int NV>
+struct RowLds {
+  uint32_t bits[(NV + 7) / 8][TH];              // four bits a vector
+  uint32_t tiles[TH / 64][(NV + 31) / 32];      // vectors of a wave with a bit set
+  // the waves' sums, of two rows in turn: a wave may write its next row's
+  // before another has read this one's
+  float m[2][TH / 64];
+  double D[2][TH / 64];
+  uint32_t ticket[2];
+};
+
+// Slot j of a thread holds the vector of tile j - (NV - tiles): a row's last
+// tile, the only one that can reach past it, is always in the last slot.  There
+// `over` elements of a vector lie past the row: the row's last whole vector is
+// read in its place and moved down.
+template <class E, class G, int TH, int NV, bool TAIL, int WAVES>
+__global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, int tiles) {
+  static_assert(E::EPV == 4, "one gradient vector per vector");
+  using vec = typename E::vec;
+  using raw = typename E::raw;
+  constexpr int TILE = TH * 4, W = TH / 64, CH = 4;
+  __shared__ RowLds<TH, NV> s;
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int j0 = NV - tiles;
+  const int vlast = (tiles - 1) * TILE + t * 4;
+  const int over = min(max(vlast + 4 - a.V, 0), 4);
+  const auto row_at = [&](int64_t u) {
+    int n, k;
+    unit_of(a, u, &n, &k);
+    return student_row<E>(a, n, k);
+  };
+  // (a uniform base and the thread's offset: no address registers per slot)
+  const auto load = [&](const raw* row, int j, int jp, int step) {
+    if (j == NV - 1) return load_vec<E>(row + (over > 0 ? a.V - 4 : vlast));
+    const char* base = reinterpret_cast<const char*>(row + static_cast<int64_t>((j - jp) * step));
+    return load_any(reinterpret_cast<const typename E::any*>(base + t * static_cast<uint32_t>(sizeof(vec))));
+  };
+  // the list entry of this thread (TAIL): its token, -1 if none
+  const auto entry = [&](int64_t u) {
+    int n, k;
+    unit_of(a, u, &n, &k);
+    return TAIL && t < a.M ? a.ids[list_of(a, n, k) + t] : -1;
+  };
+  // the bits of a token: slot, thread and element
+  const auto mark = [&](int id, bool set) {
+    if (!TAIL || id < 0 || id >= a.V) return;
+    const int j = id / TILE + j0, o = id % TILE;
+    if (set) {
+      atomicOr(&s.bits[j >> 3][o >> 2], 1u << ((j & 7) * 4 + (o & 3)));
+      atomicOr(&s.tiles[o >> 8][j >> 5], 1u << (j & 31));
+    } else {
+      s.bits[j >> 3][o >> 2] = 0;
+      s.tiles[o >> 8][j >> 5] = 0;
+    }
+  };
+  const auto taken = [&](uint32_t i) { return static_cast<int64_t>(a.order[i]); };
+  const uint32_t units = static_cast<uint32_t>(a.N) * static_cast<uint32_t>(a.K);
+  const uint32_t live = a.head[0];
+  uint32_t i = blockIdx.x, in = i + gridDim.x;  // this row and the next one
+  int turn = 0;
+  vec w[NV];
+  int id = -1;
+  if (i < live) {
+    const int64_t u = taken(i);
+    const raw* row = row_at(u);
+    const int jp = opaque_scalar(j0);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j >= jp) w[j] = load(row, j, jp, TILE);
+    id = entry(u);
+  }
+  if (TAIL) {
+#pragma unroll
+    for (int g = 0; g < (NV + 7) / 8; ++g) s.bits[g][t] = 0;
+    if (t < W * ((NV + 31) / 32)) (&s.tiles[0][0])[t] = 0;
+    __syncthreads();
+    mark(id, true);
+    __syncthreads();
+  }
+#pragma unroll 1
+  while (i < live) {
+    const int64_t u = taken(i);
+    // the row after the next one, so that no load waits for a ticket (nor the ticket
+    // for the stores before it: its value is taken behind the row's sums)
+    uint32_t drawn = 0;
+    if (t == 0) drawn = atomicAdd(a.head + 1, 1u);
+    // behind the last row the loads go on, all of them from the row's first vectors:
+    // a branch around each would make the compiler wait there for all loads and stores
+    const bool more = in < live;
+    const int64_t un = more ? taken(in) : u;
+    typename G::raw* out = static_cast<typename G::raw*>(a.grad) + u * a.V;
+    w[NV - 1] = RowVec<E>::shift(w[NV - 1], over);
+    uint32_t hits[(NV + 31) / 32];
+#pragma unroll
+    for (int g = 0; g < (NV + 31) / 32; ++g) hits[g] = TAIL ? __builtin_amdgcn_readfirstlane(s.tiles[wave][g]) : 0;
+    // a running reference over CH vectors at a time; float32 sums of 4 CH
+    float ref = -INFINITY;
+    double D = 0.0;
+    {
+      const int jp = opaque_scalar(j0);
+#pragma unroll
+      for (int c = 0; c < NV; c += CH) {
+        if (c + CH > jp) {
+          float mx = -INFINITY;
+          float x[CH][4];
+#pragma unroll
+          for (int q = 0; q < CH; ++q) {
+            const int j = c + q;
+            if (j >= NV) continue;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[q][k] = -INFINITY;
+            if (j >= jp) {
+              E::widen(w[j], x[q]);
+              if (TAIL && ((hits[j >> 5] >> (j & 31)) & 1u)) {
+                const uint32_t b = s.bits[j >> 3][t] >> ((j & 7) * 4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if ((b >> k) & 1u) x[q][k] = -INFINITY;
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx = max_nan(mx, x[q][k]);
+          }
+          const float nr = max_nan(ref, mx);
+          if (nr != -INFINITY) {
+            float sum = 0.f;
+#pragma unroll
+            for (int q = 0; q < CH; ++q)
+              if (c + q < NV) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum += scaled_exp(x[q][k], a.s_hi, a.s_lo, nr);
+              }
+            if (ref != -INFINITY && nr != ref) D *= static_cast<double>(scaled_exp(ref, a.s_hi, a.s_lo, nr));
+            D += static_cast<double>(sum);
+            ref = nr;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) RowVec<E>::hide(w[j]);
+    const float mw = wave_max(ref);
+    if (D == D && ref != -INFINITY) D *= static_cast<double>(scaled_exp(ref, a.s_hi, a.s_lo, mw));
+    D = wave_sum(D);
+    if (lane == 0) {
+      s.m[turn][wave] = mw;
+      s.D[turn][wave] = D;
+    }
+    if (t == 0) s.ticket[turn] = drawn;
+    const int id_next = more ? entry(un) : -1;
+    __syncthreads();
+    i = in;
+    in = __builtin_amdgcn_readfirstlane(s.ticket[turn]);
+    float m = s.m[turn][0];
+#pragma unroll
+    for (int q = 1; q < W; ++q) m = fmaxf(m, s.m[turn][q]);
+    D = 0.0;
+#pragma unroll
+    for (int q = 0; q < W; ++q) {
+      const double d = s.D[turn][q];
+      const float mq = s.m[turn][q];
+      D += d != d ? d : (mq != -INFINITY ? d * static_cast<double>(scaled_exp(mq, a.s_hi, a.s_lo, m)) : 0.0);
+    }
+    const ListInfo li = a.info[u];
+    const DistillNorm nm = distill_norm<TAIL>(a, li, m, D);
+    const DistillCoef co = distill_coef<TAIL>(a, li, nm);
+    if (t == 0) {
+      DistillStat o;
+      o.m = m;
+      o.pad = 0.f;
+      o.D = D;
+      a.stats[u] = o;
+    }
+    if (TAIL) {
+      mark(id, false);
+      __syncthreads();
+      mark(id_next, true);  // (seen by the other waves behind the next barrier)
+    }
+    const float cu = co.nan ? __builtin_nanf("") : co.cu;
+    const raw* next = row_at(un);
+    const int step = more ? TILE : 0;
+    const int jp = opaque_scalar(j0);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (j >= jp) {
+        float x[4], g[4];
+        E::widen(w[j], x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) g[k] = cu * scaled_exp(x[k], a.s_hi, a.s_lo, co.ru);
+        if (j < NV - 1) {
+          G::template store4<true>(
+              reinterpret_cast<typename G::raw*>(reinterpret_cast<char*>(out + static_cast<int64_t>(j - jp) * TILE) +
+                                                 t * static_cast<uint32_t>(4 * sizeof(typename G::raw))),
+              g);
+        } else if (over == 0) {
+          G::template store4<true>(out + vlast, g);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            if (k < 4 - over) G::store1(out + vlast + k, g[k]);
+        }
+        w[j] = load(next, j, jp, step);
+      }
+    }
+    turn ^= 1;
+    id = id_next;
+    if (TAIL) __syncthreads();
+  }
+  // rows without a list: a gradient of zeros; with a data error: of NaN
+#pragma unroll 1
+  while (i < units) {
+    if (t == 0) s.ticket[turn] = atomicAdd(a.head + 1, 1u);
+    const int64_t u = taken(i);
+    typename G::raw* out = static_cast<typename G::raw*>(a.grad) + u * a.V;
+    const float f = a.info[u].state == 2 ? __builtin_nanf("") : 0.f;
+    const float g[4] = {f, f, f, f};
+#pragma unroll 4
+    for (int j = 0; j < tiles - 1; ++j) G::template store4<true>(out + static_cast<int64_t>(j) * TILE + t * 4, g);
+    for (int k = 0; k < 4; ++k)
+      if (vlast + k < a.V) G::store1(out + vlast + k, f);
+    __syncthreads();
+    i = in;
+    in = __builtin_amdgcn_readfirstlane(s.ticket[turn]);
+    turn ^= 1;
+  }
+}
+
+// The listed tokens' gradients of one position, by one wave of PER entries a lane.
+template <class E, class G, int PER>
+__device__ __forceinline__ void distill_listed(const DistillArgs& a, const ListInfo& li, const DistillNorm& nm,
+                                               const DistillCoef& co, int64_t u) {
+  const int lane = threadIdx.x & 63;
+  int n, k;
+  unit_of(a, u, &n, &k);
+  const int64_t at = list_of(a, n, k);
+  const typename E::raw* row = student_row<E>(a, n, k);
+  typename G::raw* out = static_cast<typename G::raw*>(a.grad) + u * a.V;
+  int id[PER];
+  float z[PER];
+  double p[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * 64 + lane;
+    id[i] = j < a.M ? a.ids[at + j] : -1;
+    const float t = j < a.M ? a.vals[at + j] : 0.f;
+    z[i] = id[i] >= 0 ? E::one(row + id[i]) : 0.f;
+    p[i] = id[i] >= 0 ? list_prob(a, li, t) : 0.0;
+  }
+  if (li.again) {
+    double sum[PER] = {};
+    for (int j = 0; j < a.M; ++j) {
+      int oid = id[0];
+      double op = p[0];
+#pragma unroll
+      for (int i = 1; i < PER; ++i) {
+        oid = (j >> 6) == i ? id[i] : oid;
+        op = (j >> 6) == i ? p[i] : op;
+      }
+      oid = __builtin_amdgcn_readlane(oid, j & 63);
+      op = dpp::lane(op, j & 63);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sum[i] += oid == id[i] ? op : 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) p[i] = sum[i];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (id[i] >= 0) {
+      // (entries of one token write the same value)
+      G::store1(out + id[i], co.cl * scaled_exp(z[i], a.s_hi, a.s_lo, nm.M) - static_cast<float>(a.f * p[i]));
+    }
+}
+
+// The listed tokens' gradients and the position's loss, one wave a position.
+template <class E, class G>
+__global__ __launch_bounds__(kThreads) void distill_close_kernel(DistillArgs a) {
+  const int64_t u = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  if (u >= static_cast<int64_t>(a.N) * a.K) return;
+  const ListInfo li = a.info[u];
+  const DistillNorm nm = combine_distill(a, li, u);
+  const DistillCoef co = distill_coef<true>(a, li, nm);
+  if (li.state == 1 && !co.nan) {
+    if (a.M <= 64) distill_listed<E, G, 1>(a, li, nm, co, u);
+    else if (a.M <= 128) distill_listed<E, G, 2>(a, li, nm, co, u);
+    else distill_listed<E, G, kListMax / 64>(a, li, nm, co, u);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    const double L = distill_loss_of(a, li, nm);
+    a.part[u] = L;
+    if (a.per_step) a.per_step[u] = static_cast<float>(L);
+  }
 }
 
 // loss = scale / K times the sum of the per-step losses, in a fixed order.
-__global__ __launch_bounds__(kThreads) void distill_loss_kernel(const double* __restrict__ part, int64_t units,
-                                                                double scale, float* loss) {
-  __shared__ RedLds<1> s;
-  double v[1] = {0.0};
-  for (int64_t i = threadIdx.x; i < units; i += kThreads) v[0] += part[i];
-  wg_sum(v, s);
-  if (threadIdx.x == 0) *loss = static_cast<float>(v[0] * scale);
+constexpr int kLossThreads = 1024;
+__global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const double* __restrict__ part, int64_t units,
+                                                                    double scale, float* loss) {
+  __shared__ double wsum[kLossThreads / 64];
+  double v = 0.0;
+  int64_t i = threadIdx.x;
+  for (; i + 3 * kLossThreads < units; i += 4 * kLossThreads) {
+    double p[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) p[u] = part[i + u * kLossThreads];
+    v += (p[0] + p[1]) + (p[2] + p[3]);
+  }
+  for (; i < units; i += kLossThreads) v += part[i];
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) wsum[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    v = wave_sum(threadIdx.x < kLossThreads / 64 ? wsum[threadIdx.x] : 0.0);
+    if (threadIdx.x == 0) *loss = static_cast<float>(v * scale);
+  }
 }
 
 }  // namespace sv

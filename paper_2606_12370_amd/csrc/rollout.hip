@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstddef>
 #include <cstdint>
+#include <type_traits>
 
 #include "specverify_rollout.h"
 #include "sv_device.h"
@@ -84,7 +85,7 @@ spec_status launch_top(const sv::TopArgs& a, hipStream_t s) {
 
 // ---- distillation -------------------------------------------------------------------
 struct DistillLayout {
-  size_t info = 0, stats = 0, part = 0, total = 0;
+  size_t info = 0, stats = 0, part = 0, order = 0, states = 0, head = 0, total = 0;
   int C = 0;  // sub-chunks per row
 };
 DistillLayout distill_layout(int N, int K, int V, spec_dtype dt) {
@@ -95,6 +96,9 @@ DistillLayout distill_layout(int N, int K, int V, spec_dtype dt) {
   L.info = off; off = align_up(off + units * sizeof(sv::ListInfo), 256);
   L.stats = off; off = align_up(off + units * L.C * sizeof(sv::DistillStat), 256);
   L.part = off; off = align_up(off + units * sizeof(double), 256);
+  L.order = off; off = align_up(off + units * sizeof(int32_t), 256);
+  L.states = off; off = align_up(off + units * sizeof(int32_t), 256);
+  L.head = off; off = align_up(off + 2 * sizeof(uint32_t), 256);
   L.total = off;
   return L;
 }
@@ -108,10 +112,61 @@ bool distill_sizes_ok(int N, int K, int V, int M) {
 template <class E> struct Quad { using type = E; };
 template <> struct Quad<sv::BF16> { using type = sv::BF16H; };
 
+constexpr int64_t kRowBytes = 160000000;      // logits from which rows are held, and
+constexpr int64_t kLongRowBytes = 240000000;  // where a row takes a CU's registers
+constexpr int kRowCus = 256;  // of an MI355X: the launch holds what they hold at once
+
+// Rows of up to NV vectors of four logits a thread, WAVES waves per SIMD.
+template <class E, class G, bool TAIL, int TH, int NV, int WAVES>
+spec_status launch_distill_rows(sv::DistillArgs a, hipStream_t s) {
+  using Q = typename Quad<E>::type;
+  const int64_t units = int64_t{a.N} * a.K;
+  const int64_t lists = ceil_div(units, sv::kWaves);
+  a.C = 1;
+  const int tiles = static_cast<int>(ceil_div(a.V, TH * 4));
+  const int64_t wgs = std::min(units, int64_t{kRowCus} * (WAVES * 4 * 64 / TH));
+  hipLaunchKernelGGL(sv::distill_lists_kernel<Q>, groups(lists), dim3(sv::kThreads), 0, s, a);
+  // (the first two rows of a workgroup go by its number)
+  hipLaunchKernelGGL(sv::distill_order_kernel, dim3(1), dim3(sv::kOrderThreads), 0, s, a,
+                     static_cast<uint32_t>(2 * wgs));
+  void (*k)(sv::DistillArgs, int) = sv::distill_row_kernel<Q, G, TH, NV, TAIL, WAVES>;
+  hipLaunchKernelGGL(k, groups(wgs), dim3(TH), 0, s, a, tiles);
+  hipLaunchKernelGGL((sv::distill_close_kernel<Q, G>), groups(lists), dim3(sv::kThreads), 0, s, a);
+  hipLaunchKernelGGL(sv::distill_loss_kernel, dim3(1), dim3(sv::kLossThreads), 0, s, static_cast<const double*>(a.part),
+                     units, a.loss_scale, a.loss);
+  return launched();
+}
+
 template <class E, bool TAIL, class G>
 spec_status launch_distill(const sv::DistillArgs& a, hipStream_t s) {
   const int64_t units = int64_t{a.N} * a.K, nsub = units * a.C;
   const int64_t lists = ceil_div(units, sv::kWaves);
+  if (a.grad && a.V >= 4) {
+    // Rows held in registers: a row's vectors take 38 of a thread's 96 registers, 76
+    // of 128 or 152 of 256.  Small workgroups, several to a CU, keep more rows in
+    // different phases (K = 3 bfloat16, a float32 gradient, us a call with 256 / 512
+    // threads: N = 4000, V = 16000 299 / 341, V = 32000 527 / 554, N = 2000, V = 65536
+    // 507 / 526); the longest rows take a CU's registers (N = 4096, V = 151936 with 512 /
+    // 1024 threads 2.37 / 2.53 ms).
+    // Only for as many bytes of logits as the last-level cache no longer holds for
+    // the second read of the other passes.  Rows, megabytes, us a call held / read
+    // again: V = 151936 bfloat16 592 180 172 / 157, 723 220 182 / 189, 1316 400 325 /
+    // 334, 2632 800 581 / 649; V = 65536 1068 140 122 / 116, 1373 180 147 / 157, 6103 800
+    // 510 / 653; V = 32000 1562 100 97 / 86, 2187 140 123 / 119, 2812 180 151 / 172, 12500
+    // 800 537 / 738; V = 16000 4375 140 136 / 135, 25000 800 599 / 801; V = 8000 8750 140
+    // 183 / 159, 50000 800 941 / 888; float32 V = 70000 642 180 115 / 103, 928 260 147 /
+    // 141, 1142 320 174 / 195; V = 32000 1093 140 86 / 89, 6250 800 332 / 515.
+    const int64_t bytes = units * a.V * static_cast<int64_t>(sizeof(typename E::raw));
+    constexpr int F = std::is_same<E, sv::F32>::value ? 2 : 1;  // registers of a vector
+    const int64_t vecs = ceil_div(a.V, 4);
+    if (bytes >= kRowBytes && vecs > 10 / F * 256 && vecs <= 76 / F * 256) {
+      if (vecs <= 19 / F * 256) return launch_distill_rows<E, G, TAIL, 256, 19 / F, 5>(a, s);
+      if (vecs <= 38 / F * 256) return launch_distill_rows<E, G, TAIL, 256, 38 / F, 4>(a, s);
+      return launch_distill_rows<E, G, TAIL, 256, 76 / F, 2>(a, s);
+    }
+    if (bytes >= kLongRowBytes && vecs > 76 / F * 256 && vecs <= 76 / F * 512)
+      return launch_distill_rows<E, G, TAIL, 512, 76 / F, 2>(a, s);
+  }
   hipLaunchKernelGGL((sv::distill_stats_kernel<E, TAIL>), groups(lists + ceil_div(nsub, sv::kWaves)),
                      dim3(sv::kThreads), 0, s, a, static_cast<int>(lists), nsub);
   if (a.grad) {
@@ -121,7 +176,7 @@ spec_status launch_distill(const sv::DistillArgs& a, hipStream_t s) {
   } else {
     hipLaunchKernelGGL(sv::distill_norm_kernel, groups(lists), dim3(sv::kThreads), 0, s, a);
   }
-  hipLaunchKernelGGL(sv::distill_loss_kernel, dim3(1), dim3(sv::kThreads), 0, s, static_cast<const double*>(a.part),
+  hipLaunchKernelGGL(sv::distill_loss_kernel, dim3(1), dim3(sv::kLossThreads), 0, s, static_cast<const double*>(a.part),
                      units, a.loss_scale, a.loss);
   return launched();
 }
@@ -254,6 +309,9 @@ spec_status spec_distill_loss_fwd_bwd(const void* draft_logits, int64_t d_stride
   a.info = reinterpret_cast<sv::ListInfo*>(ws + L.info);
   a.stats = reinterpret_cast<sv::DistillStat*>(ws + L.stats);
   a.part = reinterpret_cast<double*>(ws + L.part);
+  a.order = reinterpret_cast<int32_t*>(ws + L.order);
+  a.states = reinterpret_cast<int32_t*>(ws + L.states);
+  a.head = reinterpret_cast<uint32_t*>(ws + L.head);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool tail = teacher_logz != nullptr;
   if (dtype == SPEC_BF16)

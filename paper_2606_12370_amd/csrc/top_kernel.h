@@ -111,7 +111,7 @@ template <bool SHORT, bool HELD = true>
 __device__ __forceinline__ int top_select(TopLds& s, int n, int M, bool exact, uint32_t* least) {
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   uint64_t prefix = 0, mask = 0;
-  uint32_t need = static_cast<uint32_t>(M);
+  uint32_t need = static_cast<uint32_t>(M), count = 0;
   int shift = 56;
   constexpr int PER = kTopCap / kThreads;
   uint64_t key[HELD ? PER : 1];
@@ -154,7 +154,7 @@ __device__ __forceinline__ int top_select(TopLds& s, int n, int M, bool exact, u
     prefix |= static_cast<uint64_t>(s.sel_digit) << shift;
     mask |= uint64_t{255} << shift;
     need = s.sel_need;
-    const uint32_t count = s.sel_count;  // keys of the prefix
+    count = s.sel_count;  // keys of the prefix
     if (count == need || shift == 0) break;
     shift -= 8;
     if (SHORT && shift == 40) {
@@ -181,7 +181,7 @@ __device__ __forceinline__ int top_select(TopLds& s, int n, int M, bool exact, u
     }
   }
   *least = static_cast<uint32_t>(prefix >> 32);
-  return static_cast<int>(s.kept);
+  return M - static_cast<int>(need) + static_cast<int>(count);  // (not s.kept, which the caller may already reset)
 }
 
 // The n candidates of s.buf sorted, the M largest of them (largest first) in its

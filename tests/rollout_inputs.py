@@ -61,8 +61,9 @@ def check_distill(got, z, ids, values, logz, T, kind, scale=1.0):
     step_lim = U * ref["step_err"] + U * np.abs(R) + tiny
     if per is not None:
         close(f64(per), R, step_lim)
-    close(f64(loss), np.array([ref["loss"]]),
-          abs(scale) * (U * ref["step_err"]).mean(axis=1).sum() + U * abs(ref["loss"]) + tiny)
+    if loss is not None:
+        close(f64(loss), np.array([ref["loss"]]),
+              abs(scale) * (U * ref["step_err"]).mean(axis=1).sum() + U * abs(ref["loss"]) + tiny)
     if grad is not None:
         close(f64(grad), ref["grad"], U * ref["grad_err"] + HALF[grad.dtype] * np.abs(ref["grad"])
               + tiny * (1 + ref["grad_unit"][..., None]))

@@ -200,6 +200,58 @@ def test_distill_masks(dtype):
         run_distill(z, ids, val, x)
 
 
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("N,K,V,M", [
+    (1, 1, 9001, 64), (70, 8, 3, 3), (64, 4, 4, 2), (300, 2, 4096, 256), (1100, 1, 38911, 64), (100, 3, 151936, 256),
+    # from 160 MB of logits on, half of that in float32: rows held in registers, by their length
+    (3000, 3, 10243, 20), (2700, 3, 10239, 20), (1500, 3, 19456, 64), (1400, 3, 19459, 17), (700, 3, 38912, 64),
+    (2100, 1, 38913, 256), (260, 4, 77824, 64),
+    # from 240 MB on, longer ones too
+    (800, 2, 77825, 64), (320, 5, 77830, 130), (270, 3, 151935, 33), (401, 2, 155648, 64), (160, 5, 155649, 64)])
+def test_distill_many_rows(N, K, V, M, dtype, tail):
+    """Calls of few and of many rows, each side of the sizes where the gradient
+    changes its launches, with empty lists, data errors and repeated ids among
+    them: sampled positions against the oracle, the loss against its own steps."""
+    ty = TYPES[dtype]
+    g = torch.Generator(device="cuda").manual_seed(N * K + V)
+    t = torch.randn((N, K, V), device="cuda", generator=g) * 3.0
+    v, i = torch.topk(t, min(M, V), dim=-1)
+    ids, val = i.to(torch.int32), v.clone()
+    lz = torch.logsumexp(t / 1.5, -1)
+    z = (t + torch.randn((N, K, V), device="cuda", generator=g)).to(ty)
+    del t, v, i
+    pos = sorted({0, 1, 2, 3, N // 3, N // 2, N - 2, N - 1} & set(range(N)))
+    if N > 8:
+        ids[1] = -1
+        ids[2, :, 1:] = ids[2, :, :1]
+        val[2, :, 1:] -= 2.0
+        z[3, 0, V // 2] = torch.nan
+        ids[N // 3, 0, 0] = V
+        ids[N // 2, :, ::2] = -1
+        z[N // 2, K - 1, :V // 2] = -torch.inf
+    for gd in ({torch.float32, ty}):
+        loss, per, grad = binding.distill_loss_fwd_bwd(z, ids, val, lz if tail else None, temperature=1.5, scale=0.5,
+                                                       grad_dtype=gd)
+        fl, fp, _ = binding.distill_loss_fwd_bwd(z, ids, val, lz if tail else None, temperature=1.5, scale=0.5,
+                                                 want_grad=False)
+        at = torch.tensor(pos, device="cuda")
+        sub = (z[at], ids[at], val[at], lz[at] if tail else None)
+        check_distill((None, per[at], grad[at]), *sub, 1.5, "forward", 0.5)
+        check_distill((None, fp[at], None), *sub, 1.5, "forward", 0.5)
+        for l, p in ((loss, per), (fl, fp)):
+            total = 0.5 * p.double().mean(-1).sum()
+            assert torch.isnan(l).all() == torch.isnan(total)
+            if N <= 8:  # (the data errors make the others NaN)
+                assert abs(float(l) - float(total)) <= 2.0 ** -23 * (abs(float(total)) + float(p.abs().sum()))
+        # every row's gradient sums to (W + r) - W - r = 0, to within the errors of the
+        # oracle's count: with a mean |d| / T of at most 15, 2 * 15 + 6 + 33 + 2 * 15 for
+        # all of q, as much for the unlisted, 3 for p; and one rounding of sum |g| <= 2
+        s = grad.double().sum(-1).abs()
+        ok = ~torch.isnan(per)
+        assert (s[ok] <= 0.5 / (K * 1.5) * (201 * 2.0 ** -24 + 2 * (2.0 ** -24 if gd == torch.float32 else 2.0 ** -8))).all()
+
+
 @pytest.mark.parametrize("dtype", DT)
 def test_distill_strides(dtype):
     """Slices: the first K of K + 1 steps of the lists, padded offset logits, a
