@@ -401,6 +401,8 @@ __global__ __launch_bounds__(kThreads) void distill_lists_kernel(DistillArgs a) 
 // The rows in the order in which distill_row takes them: those with a list first
 // (one workgroup; each thread sorts a run of consecutive rows).
 constexpr int kOrderThreads = 1024;
+// rows that a workgroup of distill_row takes by its number before it draws tickets
+constexpr int rows_ahead(bool tail) { return tail ? 3 : 2; }
 __global__ __launch_bounds__(kOrderThreads) void distill_order_kernel(DistillArgs a, uint32_t first_ticket) {
   __shared__ int wsum[kOrderThreads / 64];
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
@@ -655,10 +657,27 @@ __device__ __forceinline__ int opaque_scalar(int v) {
   return v;
 }
 
+// A value at a uniform address that an earlier launch wrote, by scalar loads: they
+// do not wait in the order of the vector loads and stores.
+template <class T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  static_assert(sizeof(T) % 4 == 0, "whole words");
+  typedef const uint32_t __attribute__((address_space(4)))* words;
+  struct Raw {
+    uint32_t w[sizeof(T) / 4];
+  } r;
+  words c = (words)(reinterpret_cast<uintptr_t>(p));
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(T) / 4; ++i) r.w[i] = c[i];
+  return __builtin_bit_cast(T, r);
+}
+
 template <int TH, int NV>
 struct RowLds {
-  uint32_t bits[(NV + 7) / 8][TH];              // four bits a vector
-  uint32_t tiles[TH / 64][(NV + 31) / 32];      // vectors of a wave with a bit set
+  // (TAIL) of three rows in turn, so that one barrier a row lies between each
+  // setting, reading and clearing
+  uint32_t bits[3][(NV + 7) / 8][TH];          // four bits a vector
+  uint32_t tiles[3][TH / 64][(NV + 31) / 32];  // vectors of a wave with a bit set
   // the waves' sums, of two rows in turn: a wave may write its next row's
   // before another has read this one's
   float m[2][TH / 64];
@@ -693,63 +712,77 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
     return load_any(reinterpret_cast<const typename E::any*>(base + t * static_cast<uint32_t>(sizeof(vec))));
   };
   // the list entry of this thread (TAIL): its token, -1 if none
-  const auto entry = [&](int64_t u) {
+  const auto entry = [&](int u) {
+    if (!TAIL) return -1;
     int n, k;
-    unit_of(a, u, &n, &k);
-    return TAIL && t < a.M ? a.ids[list_of(a, n, k) + t] : -1;
+    unit_of(a, u < 0 ? 0 : u, &n, &k);
+    const int v = a.ids[list_of(a, n, k) + (t < a.M ? t : 0)];  // (no branch around the load)
+    return u >= 0 && t < a.M ? v : -1;
   };
   // the bits of a token: slot, thread and element
-  const auto mark = [&](int id, bool set) {
+  const auto mark = [&](int ring, int id, bool set) {
     if (!TAIL || id < 0 || id >= a.V) return;
     const int j = id / TILE + j0, o = id % TILE;
     if (set) {
-      atomicOr(&s.bits[j >> 3][o >> 2], 1u << ((j & 7) * 4 + (o & 3)));
-      atomicOr(&s.tiles[o >> 8][j >> 5], 1u << (j & 31));
+      atomicOr(&s.bits[ring][j >> 3][o >> 2], 1u << ((j & 7) * 4 + (o & 3)));
+      atomicOr(&s.tiles[ring][o >> 8][j >> 5], 1u << (j & 31));
     } else {
-      s.bits[j >> 3][o >> 2] = 0;
-      s.tiles[o >> 8][j >> 5] = 0;
+      s.bits[ring][j >> 3][o >> 2] = 0;
+      s.tiles[ring][o >> 8][j >> 5] = 0;
     }
   };
-  const auto taken = [&](uint32_t i) { return static_cast<int64_t>(a.order[i]); };
   const uint32_t units = static_cast<uint32_t>(a.N) * static_cast<uint32_t>(a.K);
-  const uint32_t live = a.head[0];
-  uint32_t i = blockIdx.x, in = i + gridDim.x;  // this row and the next one
+  const uint32_t live = uniform_load(a.head);
+  // places in the order and rows (-1: none) of this row, the next one and (TAIL) the
+  // one after: each load on the way to a row's bits has a row's time to arrive
+  const auto taken = [&](uint32_t i) {
+    const int v = uniform_load(a.order + (i < units ? i : 0));
+    return i < live ? v : -1;
+  };
+  uint32_t i = blockIdx.x, in = i + gridDim.x, ia = in + gridDim.x;
+  int u = taken(i), un = taken(in), ua = TAIL ? taken(ia) : -1;
+  const auto advance = [&](uint32_t drawn, int row) {
+    i = in;
+    u = un;
+    in = TAIL ? ia : drawn;
+    un = TAIL ? ua : row;
+    ia = drawn;
+    ua = row;
+  };
   int turn = 0;
   vec w[NV];
-  int id = -1;
   if (i < live) {
-    const int64_t u = taken(i);
     const raw* row = row_at(u);
     const int jp = opaque_scalar(j0);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       if (j >= jp) w[j] = load(row, j, jp, TILE);
-    id = entry(u);
   }
+  int id = entry(u), id_next = entry(un), ring = 0;
   if (TAIL) {
 #pragma unroll
-    for (int g = 0; g < (NV + 7) / 8; ++g) s.bits[g][t] = 0;
-    if (t < W * ((NV + 31) / 32)) (&s.tiles[0][0])[t] = 0;
+    for (int g = 0; g < 3 * ((NV + 7) / 8); ++g) (&s.bits[0][0][0])[g * TH + t] = 0;
+    if (t < 3 * W * ((NV + 31) / 32)) (&s.tiles[0][0][0])[t] = 0;
     __syncthreads();
-    mark(id, true);
+    mark(0, id, true);
+    mark(1, id_next, true);
     __syncthreads();
   }
 #pragma unroll 1
   while (i < live) {
-    const int64_t u = taken(i);
-    // the row after the next one, so that no load waits for a ticket (nor the ticket
-    // for the stores before it: its value is taken behind the row's sums)
+    // (the ticket's value is taken behind the row's sums, so that it does not wait for
+    // the stores before it)
     uint32_t drawn = 0;
     if (t == 0) drawn = atomicAdd(a.head + 1, 1u);
+    int id_after = entry(ua);
     // behind the last row the loads go on, all of them from the row's first vectors:
     // a branch around each would make the compiler wait there for all loads and stores
     const bool more = in < live;
-    const int64_t un = more ? taken(in) : u;
-    typename G::raw* out = static_cast<typename G::raw*>(a.grad) + u * a.V;
+    typename G::raw* out = static_cast<typename G::raw*>(a.grad) + static_cast<int64_t>(u) * a.V;
     w[NV - 1] = RowVec<E>::shift(w[NV - 1], over);
     uint32_t hits[(NV + 31) / 32];
 #pragma unroll
-    for (int g = 0; g < (NV + 31) / 32; ++g) hits[g] = TAIL ? __builtin_amdgcn_readfirstlane(s.tiles[wave][g]) : 0;
+    for (int g = 0; g < (NV + 31) / 32; ++g) hits[g] = TAIL ? __builtin_amdgcn_readfirstlane(s.tiles[ring][wave][g]) : 0;
     // a running reference over CH vectors at a time; float32 sums of 4 CH
     float ref = -INFINITY;
     double D = 0.0;
@@ -769,7 +802,7 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
             if (j >= jp) {
               E::widen(w[j], x[q]);
               if (TAIL && ((hits[j >> 5] >> (j & 31)) & 1u)) {
-                const uint32_t b = s.bits[j >> 3][t] >> ((j & 7) * 4);
+                const uint32_t b = s.bits[ring][j >> 3][t] >> ((j & 7) * 4);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                   if ((b >> k) & 1u) x[q][k] = -INFINITY;
@@ -804,10 +837,11 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
       s.D[turn][wave] = D;
     }
     if (t == 0) s.ticket[turn] = drawn;
-    const int id_next = more ? entry(un) : -1;
+    asm volatile("" : "+v"(id_after));  // (arrived: nothing but the row's vectors is in flight below)
     __syncthreads();
-    i = in;
-    in = __builtin_amdgcn_readfirstlane(s.ticket[turn]);
+    const uint32_t drawn_now = __builtin_amdgcn_readfirstlane(s.ticket[turn]);
+    const int row_drawn = taken(drawn_now);
+    mark(ring, id, false);
     float m = s.m[turn][0];
 #pragma unroll
     for (int q = 1; q < W; ++q) m = fmaxf(m, s.m[turn][q]);
@@ -818,7 +852,7 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
       const float mq = s.m[turn][q];
       D += d != d ? d : (mq != -INFINITY ? d * static_cast<double>(scaled_exp(mq, a.s_hi, a.s_lo, m)) : 0.0);
     }
-    const ListInfo li = a.info[u];
+    const ListInfo li = uniform_load(a.info + u);
     const DistillNorm nm = distill_norm<TAIL>(a, li, m, D);
     const DistillCoef co = distill_coef<TAIL>(a, li, nm);
     if (t == 0) {
@@ -828,13 +862,8 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
       o.D = D;
       a.stats[u] = o;
     }
-    if (TAIL) {
-      mark(id, false);
-      __syncthreads();
-      mark(id_next, true);  // (seen by the other waves behind the next barrier)
-    }
     const float cu = co.nan ? __builtin_nanf("") : co.cu;
-    const raw* next = row_at(un);
+    const raw* next = row_at(more ? un : u);
     const int step = more ? TILE : 0;
     const int jp = opaque_scalar(j0);
 #pragma unroll
@@ -860,24 +889,28 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
       }
     }
     turn ^= 1;
+    // the bits of the row after the next one, behind the clearing of the same buffer
+    // by one barrier and before their reading by another
+    mark(ring == 0 ? 2 : ring - 1, id_after, true);
+    ring = ring == 2 ? 0 : ring + 1;
     id = id_next;
-    if (TAIL) __syncthreads();
+    id_next = id_after;
+    advance(drawn_now, row_drawn);
   }
   // rows without a list: a gradient of zeros; with a data error: of NaN
 #pragma unroll 1
   while (i < units) {
     if (t == 0) s.ticket[turn] = atomicAdd(a.head + 1, 1u);
-    const int64_t u = taken(i);
-    typename G::raw* out = static_cast<typename G::raw*>(a.grad) + u * a.V;
-    const float f = a.info[u].state == 2 ? __builtin_nanf("") : 0.f;
+    const int64_t v = a.order[i];
+    typename G::raw* out = static_cast<typename G::raw*>(a.grad) + v * a.V;
+    const float f = a.info[v].state == 2 ? __builtin_nanf("") : 0.f;
     const float g[4] = {f, f, f, f};
 #pragma unroll 4
     for (int j = 0; j < tiles - 1; ++j) G::template store4<true>(out + static_cast<int64_t>(j) * TILE + t * 4, g);
     for (int k = 0; k < 4; ++k)
       if (vlast + k < a.V) G::store1(out + vlast + k, f);
     __syncthreads();
-    i = in;
-    in = __builtin_amdgcn_readfirstlane(s.ticket[turn]);
+    advance(__builtin_amdgcn_readfirstlane(s.ticket[turn]), -1);
     turn ^= 1;
   }
 }

@@ -126,9 +126,8 @@ spec_status launch_distill_rows(sv::DistillArgs a, hipStream_t s) {
   const int tiles = static_cast<int>(ceil_div(a.V, TH * 4));
   const int64_t wgs = std::min(units, int64_t{kRowCus} * (WAVES * 4 * 64 / TH));
   hipLaunchKernelGGL(sv::distill_lists_kernel<Q>, groups(lists), dim3(sv::kThreads), 0, s, a);
-  // (the first two rows of a workgroup go by its number)
   hipLaunchKernelGGL(sv::distill_order_kernel, dim3(1), dim3(sv::kOrderThreads), 0, s, a,
-                     static_cast<uint32_t>(2 * wgs));
+                     static_cast<uint32_t>(sv::rows_ahead(TAIL) * wgs));
   void (*k)(sv::DistillArgs, int) = sv::distill_row_kernel<Q, G, TH, NV, TAIL, WAVES>;
   hipLaunchKernelGGL(k, groups(wgs), dim3(TH), 0, s, a, tiles);
   hipLaunchKernelGGL((sv::distill_close_kernel<Q, G>), groups(lists), dim3(sv::kThreads), 0, s, a);
