@@ -667,29 +667,34 @@ def distill_loss_fwd_bwd(draft_logits, teacher_ids, teacher_values, teacher_logz
     lib = _lib or load_library()
     if draft_logits.dim() != 3:
         raise ValueError("draft_logits must be [N, K, V]")
-    N, K, V = draft_logits.shape
-    _check_rows(draft_logits, "draft_logits", (N, K, V))
+    shape = draft_logits.shape
+    N, K, V = shape
+    sn, sk, sv = draft_logits.stride()
+    if sv != 1:
+        raise ValueError("draft_logits: the vocabulary dimension must be contiguous")
     dev = _gpu(draft_logits, "draft_logits")
     code = _dtype_code(draft_logits)
-    if teacher_ids.dim() != 3 or teacher_ids.shape[0] != N or teacher_ids.shape[1] != K:
+    listed = teacher_ids.shape
+    if len(listed) != 3 or listed[0] != N or listed[1] != K:
         raise ValueError("teacher_ids must be [N, K, M] with N=%d, K=%d" % (N, K))
-    M = teacher_ids.shape[2]
+    M = listed[2]
     if not 1 <= M <= SPEC_MAX_LIST:
         raise ValueError("lists must have 1 to %d entries, got %d" % (SPEC_MAX_LIST, M))
     if teacher_ids.dtype != torch.int32 or teacher_values.dtype != torch.float32:
         raise ValueError("teacher_ids must be int32 and teacher_values float32")
-    if teacher_values.shape != teacher_ids.shape or teacher_values.stride()[:2] != teacher_ids.stride()[:2]:
+    ln, lk, lm = teacher_ids.stride()
+    vn, vk, vm = teacher_values.stride() if teacher_values.dim() == 3 else (-1, -1, -1)
+    if teacher_values.shape != listed or vn != ln or vk != lk:
         raise ValueError("teacher_values must have the shape and strides of teacher_ids")
-    if M > 1 and (teacher_ids.stride(2) != 1 or teacher_values.stride(2) != 1):
+    if M > 1 and (lm != 1 or vm != 1):
         raise ValueError("teacher_ids, teacher_values: the list dimension must be contiguous")
     zp, zn, zk = None, 0, 0
     if teacher_logz is not None:
         if teacher_logz.dtype != torch.float32 or tuple(teacher_logz.shape) != (N, K):
             raise ValueError("teacher_logz must be a float32 [N, K] tensor")
         zp, zn, zk = teacher_logz.data_ptr(), teacher_logz.stride(0), teacher_logz.stride(1)
-    for t, name in ((teacher_ids, "teacher_ids"), (teacher_values, "teacher_values"), (teacher_logz, "teacher_logz")):
-        if t is not None and t.device != dev:
-            raise ValueError("%s is on %s, expected %s" % (name, t.device, dev))
+    if teacher_ids.device != dev or teacher_values.device != dev or (zp is not None and teacher_logz.device != dev):
+        raise ValueError("the teacher's lists must be on %s" % dev)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     per_step = torch.empty((N, K), dtype=torch.float32, device=dev) if want_per_step else None
     grad, gcode = None, SPEC_F32
@@ -700,20 +705,18 @@ def distill_loss_fwd_bwd(draft_logits, teacher_ids, teacher_values, teacher_logz
             raise TypeError("grad_dtype must be float32 or the draft logits' dtype, got %s" % grad_dtype)
         gcode = SPEC_BF16 if grad_dtype == torch.bfloat16 else SPEC_F32
         if grad_out is None:
-            grad = torch.empty((N, K, V), dtype=grad_dtype, device=dev)
+            grad = torch.empty(shape, dtype=grad_dtype, device=dev)
         else:
             grad = grad_out
-            _check_tensor(grad, "grad_out", grad_dtype, draft_logits.shape, dev)
+            _check_tensor(grad, "grad_out", grad_dtype, shape, dev)
             a0, a1 = grad.data_ptr(), grad.data_ptr() + grad.numel() * grad.element_size()
             b0 = draft_logits.data_ptr()
-            b1 = b0 + ((N - 1) * draft_logits.stride(0) + (K - 1) * draft_logits.stride(1) + V) \
-                * draft_logits.element_size()
+            b1 = b0 + ((N - 1) * sn + (K - 1) * sk + V) * draft_logits.element_size()
             if a0 < b1 and b0 < a1:
                 raise ValueError("grad_out overlaps draft_logits")
     _call("spec_distill_loss_fwd_bwd", lib.spec_distill_loss_fwd_bwd,
           lib.spec_distill_workspace_size(N, K, V, M, code), ws, dev,
-          (draft_logits.data_ptr(), draft_logits.stride(0), draft_logits.stride(1), code, N, K, V,
-           teacher_ids.data_ptr(), teacher_values.data_ptr(), teacher_ids.stride(0), teacher_ids.stride(1), M,
+          (draft_logits.data_ptr(), sn, sk, code, N, K, V, teacher_ids.data_ptr(), teacher_values.data_ptr(), ln, lk, M,
            zp, zn, zk, float(temperature), DISTILL_KINDS[kind] if isinstance(kind, str) else int(kind), float(scale),
            loss.data_ptr(), None if per_step is None else per_step.data_ptr(),
            None if grad is None else grad.data_ptr(), gcode))
@@ -738,7 +741,9 @@ def verify_probs(target_probs, draft_probs, draft_ids, accept_uniforms, sample_u
         raise ValueError("target_probs must be [B, K+1, V]")
     B, K1, V = target_probs.shape
     K = K1 - 1
-    _check_rows(target_probs, "target_probs", (B, K1, V))
+    tb, tk, tv = target_probs.stride()
+    if tv != 1:
+        raise ValueError("target_probs: the vocabulary dimension must be contiguous")
     dev = _gpu(target_probs, "target_probs")
     code = _dtype_code(target_probs)
     dp, db, dk = None, 0, 0
@@ -771,7 +776,7 @@ def verify_probs(target_probs, draft_probs, draft_ids, accept_uniforms, sample_u
             _check_tensor(out["overlap"], "out['overlap']", torch.float32, (B, K), dev)
     ov = out.get("overlap")
     _call("spec_verify_probs", lib.spec_verify_probs, lib.spec_verify_probs_workspace_size(B, K, V, code), ws, dev,
-          (target_probs.data_ptr(), target_probs.stride(0), target_probs.stride(1), dp, db, dk, code, B, K, V,
+          (target_probs.data_ptr(), tb, tk, dp, db, dk, code, B, K, V,
            ip, up, sample_uniforms.data_ptr(), lp, out["accept_len"].data_ptr(), out["emitted"].data_ptr(),
            None if ov is None or K == 0 else ov.data_ptr()))
     return out

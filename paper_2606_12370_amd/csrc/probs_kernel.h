@@ -1,7 +1,8 @@
 // probs_kernel.h — chain rejection-sampling verification from given
 // probabilities and given uniforms (paper Sec. 2.2 Eq. reject_sample, App.
-// G.1 Alg. rs_multinomial), in two launches:
+// G.1 Alg. rs_multinomial), in two launches, or three in large calls:
 //
+//   0 probs_decide  (large calls) one wave per batch row: the accept tests.
 //   1 probs_pass    one wave per (batch row, sub-chunk) of the emitting step,
 //                   with overlaps per (batch row, step, sub-chunk): the accept
 //                   tests from the gathered p(x_i), q(x_i), then the
@@ -24,10 +25,10 @@
 
 namespace sv {
 
-constexpr int kProbsVec = 16;  // vectors per lane of a sub-chunk (one wave)
-
+// Elements of a sub-chunk (one wave), read in four steps of 16 a lane.
+constexpr int kProbsSub = 4096;
 template <class E>
-constexpr int probs_sub() { return kProbsVec * 64 * E::EPV; }
+constexpr int probs_step() { return 16 / E::EPV; }
 
 struct ProbsArgs {
   const void* p; int64_t psb, psk;  // target probabilities [B, K + 1, V]
@@ -41,6 +42,7 @@ struct ProbsArgs {
   int32_t* accept_len;
   int32_t* emitted;
   float* overlap;                   // [B, K] or nullptr
+  struct ProbsDecision* decision;   // [B] or nullptr: every wave takes the tests itself
   double* res;                      // [B][C] residual sums of the emitting step
   double* ov;                       // [B][K][C] overlap sums (with overlap and draft probabilities)
 };
@@ -51,14 +53,14 @@ __device__ __forceinline__ bool prob_ok(float p) { return p >= 0.f && p < INFINI
 struct ProbsDecision {
   int n, len;  // first rejected step (len if none), drafted tokens of the row
   int x;       // the rejected token (n < len)
-  bool bad;    // a value the decision depends on is no probability, uniform, id or length
-  float px;    // lane i < len: p_i(x_i)
+  int bad;     // a value the decision depends on is no probability, uniform, id or length
 };
 
 // The accept tests of one batch row, taken by a whole wave (lane i tests step i).
 template <class E>
 __device__ __forceinline__ ProbsDecision probs_decide(const ProbsArgs& a, int b) {
   using raw = typename E::raw;
+  if (a.decision) return a.decision[b];
   const int lane = threadIdx.x & 63;
   ProbsDecision d;
   d.len = a.lens ? a.lens[b] : a.K;
@@ -66,7 +68,6 @@ __device__ __forceinline__ ProbsDecision probs_decide(const ProbsArgs& a, int b)
   if (len_bad) d.len = 0;
   bool bad = len_bad, reject = false;
   int x = 0;
-  d.px = 0.f;
   if (lane < d.len) {
     x = a.ids[static_cast<int64_t>(b) * a.K + lane];
     const float u = a.ua[static_cast<int64_t>(b) * a.K + lane];
@@ -76,15 +77,22 @@ __device__ __forceinline__ ProbsDecision probs_decide(const ProbsArgs& a, int b)
     const float q = a.q ? E::one(static_cast<const raw*>(a.q) + b * a.qsb + lane * a.qsk + xs) : 1.f;
     bad = bad || !(u >= 0.f && u <= 1.f) || !prob_ok(p) || !prob_ok(q);
     reject = !(static_cast<double>(u) * static_cast<double>(q) < static_cast<double>(p));
-    d.px = p;
   }
   const float us = a.us[b];
   bad = bad || !(us >= 0.f && us <= 1.f);
-  d.bad = __ballot(bad) != 0;
+  d.bad = __ballot(bad) != 0 ? 1 : 0;
   const uint64_t rej = __ballot(reject);
   d.n = rej ? __builtin_ctzll(rej) : d.len;
   d.x = __builtin_amdgcn_readlane(x, d.n < 63 ? d.n : 63);
   return d;
+}
+
+template <class E>
+__global__ __launch_bounds__(kThreads) void probs_decide_kernel(ProbsArgs a, ProbsDecision* out) {
+  const int b = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (b >= a.B) return;
+  const ProbsDecision d = probs_decide<E>(a, b);
+  if ((threadIdx.x & 63) == 0) out[b] = d;
 }
 
 // Load S vectors per lane as load_span does, with 0 beyond the row.
@@ -115,7 +123,7 @@ __device__ __forceinline__ double residual(float p, float q) {
 template <class E, bool OV>
 __global__ __launch_bounds__(kThreads) void probs_pass_kernel(ProbsArgs a, int64_t units) {
   using raw = typename E::raw;
-  constexpr int EPV = E::EPV, S = 4, SUB = probs_sub<E>();
+  constexpr int EPV = E::EPV, S = probs_step<E>();
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t g = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
   if (g >= units) return;
@@ -132,11 +140,11 @@ __global__ __launch_bounds__(kThreads) void probs_pass_kernel(ProbsArgs a, int64
   const raw* prow = static_cast<const raw*>(a.p) + b * a.psb + i * a.psk;
   const raw* qrow = draft ? static_cast<const raw*>(a.q) + b * a.qsb + i * a.qsk : prow;
   const int struck = (!a.q && i < d.len) ? d.x : -1;
-  const int e0 = c * SUB;
+  const int e0 = c * kProbsSub;
   double rs = 0.0, os = 0.0;
   float lo = 0.f, hi = 0.f;
 #pragma unroll 1
-  for (int st = 0; st < kProbsVec / S; ++st) {
+  for (int st = 0; st < kProbsSub / (S * 64 * EPV); ++st) {
     const int es = e0 + st * S * 64 * EPV;
     if (es >= a.V) break;
     float x[S][EPV], y[S][EPV];
@@ -201,10 +209,10 @@ __device__ __forceinline__ double wg_excl_scan(double v, double* total, ProbsLds
 template <class E>
 __device__ __forceinline__ int probs_pick(const typename E::raw* prow, const typename E::raw* qrow, int struck, int V,
                                           int c, double base, double target, ProbsLds& s) {
-  constexpr int EPV = E::EPV, TILES = probs_sub<E>() / (kThreads * EPV);
-  static_assert(TILES == 4, "one wsum row per tile");
+  constexpr int EPV = E::EPV, TILES = kProbsSub / (kThreads * EPV);
+  static_assert(TILES <= 4, "one wsum row per tile");
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  const int e0 = c * probs_sub<E>();
+  const int e0 = c * kProbsSub;
   float x[TILES][EPV], y[TILES][EPV];
   load_probs<E, TILES, kThreads>(prow, e0, t, V, x);
   if (qrow) {
@@ -258,13 +266,13 @@ __device__ __forceinline__ int probs_pick(const typename E::raw* prow, const typ
 // the rows whose residual has no mass, whose token is drawn from p itself.
 template <class E>
 __device__ __forceinline__ double probs_sub_sum(const typename E::raw* prow, int V, int c) {
-  constexpr int EPV = E::EPV, S = 4;
+  constexpr int EPV = E::EPV, S = probs_step<E>();
   const int lane = threadIdx.x & 63;
   double rs = 0.0;
   float lo = 0.f, hi = 0.f;
 #pragma unroll 1
-  for (int st = 0; st < kProbsVec / S; ++st) {
-    const int es = c * probs_sub<E>() + st * S * 64 * EPV;
+  for (int st = 0; st < kProbsSub / (S * 64 * EPV); ++st) {
+    const int es = c * kProbsSub + st * S * 64 * EPV;
     if (es >= V) break;
     float x[S][EPV];
     load_probs<E, S, 64>(prow, es, lane, V, x);
@@ -369,7 +377,8 @@ __global__ __launch_bounds__(kThreads) void probs_finish_kernel(ProbsArgs a) {
     } else if (i >= d.len) {
       v = 0.f;
     } else if (!a.q) {
-      v = __shfl(d.px, i, 64);
+      const int x = a.ids[static_cast<int64_t>(b) * a.K + i];
+      v = E::one(static_cast<const raw*>(a.p) + b * a.psb + i * a.psk + x);
     } else {
       const double* o = a.ov + (static_cast<int64_t>(b) * a.K + i) * a.C;
       double m = 0.0;

@@ -187,13 +187,14 @@ spec_status launch_distill_grad(const sv::DistillArgs& a, spec_dtype gd, hipStre
 
 // ---- verification from probabilities --------------------------------------------------
 struct ProbsLayout {
-  size_t res = 0, ov = 0, total = 0;
+  size_t decision = 0, res = 0, ov = 0, total = 0;
   int C = 0;
 };
-ProbsLayout probs_layout(int B, int K, int V, spec_dtype dt) {
+ProbsLayout probs_layout(int B, int K, int V) {
   ProbsLayout L;
-  L.C = static_cast<int>(ceil_div(V, dt == SPEC_BF16 ? sv::probs_sub<sv::BF16>() : sv::probs_sub<sv::F32>()));
+  L.C = static_cast<int>(ceil_div(V, sv::kProbsSub));
   size_t off = 0;
+  L.decision = off; off = align_up(off + static_cast<size_t>(B) * sizeof(sv::ProbsDecision), 256);
   L.res = off; off = align_up(off + static_cast<size_t>(B) * L.C * sizeof(double), 256);
   L.ov = off; off = align_up(off + static_cast<size_t>(B) * K * L.C * sizeof(double), 256);
   L.total = off;
@@ -205,8 +206,20 @@ bool probs_sizes_ok(int B, int K, int V) {
          int64_t{B} * (K + 1) * ceil_div(V, 4096) < kMaxGroups * sv::kWaves && B < kMaxGroups;
 }
 
+// Units (waves of the pass) from which the accept tests take a launch of their own
+// instead of every wave taking its row's (us a call, with overlaps, K = 3; in the
+// pass / own launch: float32 V = 151936 B = 1 14.2 / 15.5, B = 256 (38912 units) 159 /
+// 161, B = 512 308.5 / 309.8; bfloat16 V = 262144 B = 64 (16384) 62.4 / 61.4, B = 256
+// (65536) 191 / 183, B = 1000 707 / 665; without overlaps B = 1000 (64000) 164 / 160).
+constexpr int64_t kProbsDecideUnits = 49152;
+
 template <class E>
-spec_status launch_probs(const sv::ProbsArgs& a, hipStream_t s) {
+spec_status launch_probs(sv::ProbsArgs a, sv::ProbsDecision* decision, hipStream_t s) {
+  if (int64_t{a.B} * (a.overlap ? a.K + 1 : 1) * a.C > kProbsDecideUnits) {
+    hipLaunchKernelGGL(sv::probs_decide_kernel<E>, groups(ceil_div(a.B, sv::kWaves)), dim3(sv::kThreads), 0, s, a,
+                       decision);
+    a.decision = decision;
+  }
   if (a.overlap) {
     const int64_t units = int64_t{a.B} * (a.K + 1) * a.C;
     hipLaunchKernelGGL((sv::probs_pass_kernel<E, true>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads), 0, s,
@@ -321,7 +334,7 @@ spec_status spec_distill_loss_fwd_bwd(const void* draft_logits, int64_t d_stride
 
 size_t spec_verify_probs_workspace_size(int B, int K, int V, spec_dtype dtype) {
   if (!dtype_ok(dtype) || !probs_sizes_ok(B, K, V)) return 0;
-  return probs_layout(B, K, V, dtype).total;
+  return probs_layout(B, K, V).total;
 }
 
 spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int64_t t_stride_k,
@@ -338,7 +351,7 @@ spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int6
   if (!extent_ok(target_probs, B, t_stride_b, K + 1, t_stride_k, V, esize_of(dtype)) ||
       (draft_probs && K > 0 && !extent_ok(draft_probs, B, d_stride_b, K, d_stride_k, V, esize_of(dtype))))
     return SPEC_EINVAL;
-  const ProbsLayout L = probs_layout(B, K, V, dtype);
+  const ProbsLayout L = probs_layout(B, K, V);
   if (!workspace || workspace_bytes < L.total) return SPEC_EWORKSPACE;
   if (!aligned16(workspace)) return SPEC_EINVAL;
 
@@ -353,7 +366,8 @@ spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int6
   a.res = reinterpret_cast<double*>(ws + L.res);
   a.ov = reinterpret_cast<double*>(ws + L.ov);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return dtype == SPEC_BF16 ? launch_probs<sv::BF16>(a, s) : launch_probs<sv::F32>(a, s);
+  sv::ProbsDecision* decision = reinterpret_cast<sv::ProbsDecision*>(ws + L.decision);
+  return dtype == SPEC_BF16 ? launch_probs<sv::BF16>(a, decision, s) : launch_probs<sv::F32>(a, decision, s);
 }
 
 }  // extern "C"
