@@ -229,6 +229,11 @@ __device__ __forceinline__ void top_put(TopLds& s, uint64_t hit, uint32_t base, 
   if ((hit >> (threadIdx.x & 63)) & 1) s.buf[pos] = top_key(x, i);
 }
 
+// log2(e) / T, finite also for the smallest temperatures (1 for one that is none).
+__device__ __forceinline__ float top_scale(float T) {
+  return temperature_ok(T) ? fminf(scale_of(T), 3.402823466e38f) : 1.0f;
+}
+
 // log sum exp(z / T) from the largest logit and the sum relative to it.
 __device__ __forceinline__ float top_logz(float M, float T, double D) {
   return M == -INFINITY ? -INFINITY
@@ -246,13 +251,14 @@ __device__ __forceinline__ void top_write(const TopLds& s, int n, const TopArgs&
 
 // sum of exp((x - ref) / T) over one step's logits of a thread, sc = log2(e) / T.
 // One fused multiply-add and one exponential per logit; what the product ref sc
-// loses to rounding is given back to the sum.  References whose product is not
-// finite (rows of the lowest values) take the difference first.
+// loses to rounding, at most 2^-13 where it is at most 4096, is given back to the
+// sum to first order (the second is below 4e-9).  Larger products (huge logits,
+// tiny temperatures, rows of the lowest values) take the difference first.
 template <int S, int EPV>
 __device__ __forceinline__ double top_exp_sum(const float (&x)[S][EPV], float ref, float sc) {
   const float c = ref * sc;
   float sum = 0.f;
-  if (__any(!(fabsf(c) < INFINITY))) {
+  if (__any(!(fabsf(c) <= 4096.f))) {
 #pragma unroll
     for (int j = 0; j < S; ++j)
 #pragma unroll
@@ -278,7 +284,7 @@ __global__ __launch_bounds__(kThreads, kTopWaves) void top_part_kernel(TopArgs a
   int b;
   const typename E::raw* row = row_of<E>(a.rows, static_cast<int>(r), &b);
   const float T = temperature_of(a.rows, b);
-  const float sc = temperature_ok(T) ? scale_of(T) : 1.0f;
+  const float sc = top_scale(T);
   const int lo = part * a.part;
   const int hi = a.rows.V - lo < a.part ? a.rows.V : lo + a.part;
   RawSpan<E, S, kThreads> next;
@@ -481,7 +487,7 @@ __global__ __launch_bounds__(kThreads) void top_merge_kernel(TopArgs a) {
     int b;
     (void)row_of<BF16>(a.rows, static_cast<int>(r), &b);
     const float T = temperature_of(a.rows, b);
-    const float sc = scale_of(T);
+    const float sc = top_scale(T);
     float m = -INFINITY;
     for (int p = t; p < a.P; p += 64) m = fmaxf(m, p == t ? own.m : st[p].m);
     m = wave_max(m);

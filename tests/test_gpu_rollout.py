@@ -85,6 +85,32 @@ def test_top_row_temperatures_and_strides(dtype):
     check_top(binding.top_logits(z, 50, bad), z, 50, bad.cpu().numpy())
 
 
+@pytest.mark.parametrize("dtype", DT)
+def test_top_extreme_temperatures(dtype):
+    """Temperatures from the smallest float32 to the largest: 0 at T near 0 stays 0."""
+    z = logit_rows((6, 5000), TYPES[dtype], 13)
+    z[:, 0] = 0.0
+    z[:2] = -z[:2].abs()
+    T = torch.tensor([1.4e-45, 1e-38, 1e-20, 1e-3, 1e20, 3e38], device="cuda")
+    out = binding.top_logits(z, 10, T)
+    z64 = z.double()
+    assert torch.equal(out["ids"][:, 0].long(), z64.argmax(-1))
+    want = torch.logsumexp((z64 - z64.amax(-1, keepdim=True)) / T.double()[:, None], -1) + z64.amax(-1) / T.double()
+    assert torch.allclose(out["logz"], want.float(), rtol=1e-6, atol=1e-6)
+
+
+@pytest.mark.parametrize("scale", [1e3, 1e5, 1e30])
+@pytest.mark.parametrize("dtype", DT)
+def test_top_huge_logits(dtype, scale):
+    """The product of a logit and log2(e) / T then has no fraction bits left."""
+    z = (logit_rows((3, 5000), torch.float32, 14) * scale).to(TYPES[dtype])
+    z[0] = z[0, 0]  # every term counts
+    z[1] -= 10 * scale
+    check_top(binding.top_logits(z, 20, 0.7), z, 20, np.float32(0.7))
+    T = torch.tensor([0.3, 1.0, 7.0], device="cuda")
+    check_top(binding.top_logits(z, 20, T), z, 20, T.cpu().numpy())
+
+
 # ---- distillation --------------------------------------------------------------------
 
 def run_distill(z, ids, val, lz, T=1.0, kind="forward", scale=0.75, grad_dtype=None):
@@ -305,6 +331,18 @@ def test_probs_sizes(B, K, V, dtype, draft):
     check_probs(binding.verify_probs(p, q, ids, u, us, want_overlap=False), p, q, ids, u, us)
 
 
+@pytest.mark.parametrize("B,K,V,dtype,draft", [(13000, 3, 100, "f32", True), (12500, 3, 60, "bf16", False),
+                                               (50000, 1, 20, "bf16", True), (12288, 3, 33, "f32", True),
+                                               (12289, 3, 33, "f32", True)])
+def test_probs_many_rows(B, K, V, dtype, draft):
+    """Each side of the size from which the accept tests take their own launch."""
+    p, q, ids, u, us = probs(B, K, V, TYPES[dtype], B + V, draft=draft)
+    lens = (torch.arange(B, device="cuda") * 7 % (K + 1)).to(torch.int32)
+    lens[5] = K + 1
+    check_probs(binding.verify_probs(p, q, ids, u, us, draft_lens=lens), p, q, ids, u, us, lens)
+    check_probs(binding.verify_probs(p, q, ids, u, us, want_overlap=False), p, q, ids, u, us)
+
+
 @pytest.mark.parametrize("draft", [True, False])
 @pytest.mark.parametrize("dtype", DT)
 def test_probs_ragged(dtype, draft):
@@ -429,6 +467,34 @@ def test_a_rollout_step_and_its_training_step():
     # both within their float32 sums of the same values
     assert torch.allclose(per, kps, rtol=1e-5, atol=1e-5)
     assert torch.allclose(grad, kg, rtol=1e-4, atol=1e-7)
+
+
+def test_two_rollout_threads():
+    """Calls from two host threads at once, each on its own stream."""
+    import threading
+    want = {s: [_bits(c()) for c in _calls(s)] for s in (181, 191)}
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(seed):
+        try:
+            calls = _calls(seed)
+            s = torch.cuda.Stream()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                for _ in range(5):
+                    for w, c in zip(want[seed], calls):
+                        assert all(torch.equal(x, y) for x, y in zip(w, _bits(c())))
+            s.synchronize()
+        except BaseException as e:  # noqa: BLE001 (handed to the test's thread)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(s,)) for s in want]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
 
 
 def _calls(seed):
