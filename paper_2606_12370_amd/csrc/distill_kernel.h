@@ -21,11 +21,16 @@
 // and float64 beyond.
 //
 // Launches, with a gradient of many rows that fit the registers: 1 distill_lists
-// (a wave per list), 2 distill_row (workgroups that hold whole rows), 3
-// distill_close (the listed tokens), 4 distill_loss.  Otherwise: 1 distill_stats
-// (a wave per list, and a wave per sub-chunk of the student's row), 2
-// distill_grad (a workgroup per chunk), or distill_norm without a gradient, 3
-// distill_loss.
+// (a wave per list), 2 distill_order (rows with a list first), 3 distill_row
+// (workgroups that hold whole rows), 4 distill_close (the listed tokens), 5
+// distill_loss.  Otherwise: 1 distill_stats (a wave per list, and a wave per
+// sub-chunk of the student's row), 2 distill_grad (a workgroup per chunk), or
+// distill_norm without a gradient, 3 distill_loss.
+//
+// Memory bounds the large calls.  N = 4096, K = 3, V = 151936 bfloat16, M = 64, a
+// float32 gradient: 2307 us, of which distill_row 2225 (5.0 TB/s read and
+// written; a large copy reaches 4.93), lists 34, close 46.  Without a gradient 3000
+// rows of 262144: distill_stats 277 us (5.7 TB/s).
 #pragma once
 
 #include <type_traits>
@@ -508,24 +513,31 @@ struct GradBF16 {
 
 // The gradient's coefficients: listed tokens get cl exp((z - M) / T) - f sum p,
 // unlisted ones cu exp((z - ru) / T), ru = mo (0 where every one of them is -inf).
+// (cl is a double: the difference of two terms that float32 need not hold.)
 struct DistillCoef {
-  float cl, cu, ru;
+  double cl;
+  float cu, ru;
   bool nan;
 };
 template <bool TAIL>
 __device__ __forceinline__ DistillCoef distill_coef(const DistillArgs& a, const ListInfo& li, const DistillNorm& n) {
   DistillCoef c;
   c.nan = li.state == 2 || (li.state == 1 && !norm_ok(n));
+  // (a gradient beyond float32's range ends at its largest number: a token whose
+  // exponential is 0 has 0 and not the product of 0 and an infinity)
+  const auto bounded = [](double v) {
+    return static_cast<float>(fmin(fmax(v, -3.4028234663852886e38), 3.4028234663852886e38));
+  };
   const double all = a.f * (li.W + li.r) / n.D;
-  c.cl = static_cast<float>(all);
+  c.cl = all;
   // where no unlisted token has mass, none has a gradient either
   c.cu = 0.f;
   c.ru = n.mo > -INFINITY ? n.mo : 0.f;
   if (!TAIL) {
-    c.cu = c.cl;
+    c.cu = bounded(all);
   } else if (n.mo > -INFINITY) {
     const double w = exp_of(static_cast<double>(n.mo) - static_cast<double>(n.M), a.inv_t);
-    c.cu = static_cast<float>(all * w - (li.r > 0.0 ? a.f * li.r / n.Do : 0.0));
+    c.cu = bounded(all * w - (li.r > 0.0 ? a.f * li.r / n.Do : 0.0));
   }
   return c;
 }
@@ -609,7 +621,7 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs a, i
       for (int j = 0; j < a.M; ++j)
         if (a.ids[at + j] == id) p += list_prob(a, li, a.vals[at + j]);
     }
-    G::store1(out + id, co.cl * scaled_exp(z, a.s_hi, a.s_lo, nm.M) - static_cast<float>(a.f * p));
+    G::store1(out + id, static_cast<float>(co.cl * static_cast<double>(scaled_exp(z, a.s_hi, a.s_lo, nm.M)) - a.f * p));
   }
 }
 
@@ -782,7 +794,8 @@ __global__ __launch_bounds__(TH, WAVES) void distill_row_kernel(DistillArgs a, i
     w[NV - 1] = RowVec<E>::shift(w[NV - 1], over);
     uint32_t hits[(NV + 31) / 32];
 #pragma unroll
-    for (int g = 0; g < (NV + 31) / 32; ++g) hits[g] = TAIL ? __builtin_amdgcn_readfirstlane(s.tiles[ring][wave][g]) : 0;
+    for (int g = 0; g < (NV + 31) / 32; ++g)
+      hits[g] = TAIL ? __builtin_amdgcn_readfirstlane(s.tiles[ring][wave][g]) : 0;
     // a running reference over CH vectors at a time; float32 sums of 4 CH
     float ref = -INFINITY;
     double D = 0.0;
@@ -958,7 +971,8 @@ __device__ __forceinline__ void distill_listed(const DistillArgs& a, const ListI
   for (int i = 0; i < PER; ++i)
     if (id[i] >= 0) {
       // (entries of one token write the same value)
-      G::store1(out + id[i], co.cl * scaled_exp(z[i], a.s_hi, a.s_lo, nm.M) - static_cast<float>(a.f * p[i]));
+      G::store1(out + id[i], static_cast<float>(
+                                    co.cl * static_cast<double>(scaled_exp(z[i], a.s_hi, a.s_lo, nm.M)) - a.f * p[i]));
     }
 }
 

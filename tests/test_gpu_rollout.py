@@ -292,6 +292,25 @@ def test_distill_strides(dtype):
     run_distill(shared, i, v, l)
 
 
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("rows", [3, 800])
+def test_distill_gradient_beyond_float32(rows, tail):
+    """At a temperature whose inverse float32 does not hold, tokens without mass have a gradient of 0, not NaN."""
+    V = 152000
+    z = -logit_rows((rows, 1, V), torch.bfloat16, 15).abs() - 1.0
+    z[:, 0, 5] = 0.0
+    ids = torch.tensor([5, 7], dtype=torch.int32, device="cuda").expand(rows, 1, 2).contiguous()
+    val = torch.zeros(rows, 1, 2, device="cuda")
+    lz = torch.full((rows, 1), 1.0, device="cuda") if tail else None
+    _, _, grad = binding.distill_loss_fwd_bwd(z, ids, val, lz, temperature=1e-40, kind="ce")
+    assert not torch.isnan(grad).any()
+    rest = torch.ones(V, dtype=torch.bool, device="cuda")
+    rest[[5, 7]] = False
+    if not tail:
+        assert (grad[..., rest] == 0).all()
+    assert (grad[:, 0, 5] > 0).all() and (grad[:, 0, 7] < 0).all()
+
+
 def test_distill_gradient_against_differences():
     """The gradient against central differences of the float64 loss; the first log
     Z is one of another temperature, whose probabilities sum to far more than 1."""
