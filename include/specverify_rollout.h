@@ -94,7 +94,8 @@ size_t spec_distill_workspace_size(int N, int K, int V, int M, spec_dtype dtype)
  * temperature     finite and > 0
  * loss            [1] float32 out
  * per_step        [N, K] float32 out: L_{n,k} (may be NULL)
- * grad_draft      [N, K, V] out, contiguous, of grad_dtype; NULL = forward only
+ * grad_draft      [N, K, V] out, contiguous, of grad_dtype, without overlap with
+ *                  an input; NULL = forward only
  * grad_dtype      SPEC_F32, or the draft logits' dtype (rounded once, to nearest)
  * workspace       device memory of at least spec_distill_workspace_size bytes
  * Data errors (an id >= V, a NaN among teacher_values or in teacher_logz, a

@@ -465,9 +465,8 @@ def test_probs_strides(dtype):
 
 def test_a_rollout_step_and_its_training_step():
     """Verify the drafts of a batch, record the target's top logits at the
-    temperature of training, distil the draft from the record: the loss falls
-    along its gradient, and with the whole vocabulary listed it is the forward
-    KL of the rows themselves."""
+    temperature of training, distil the draft from the record: with the whole
+    vocabulary listed that is the forward KL of the rows themselves."""
     B, K, V, M = 6, 3, 200, 200
     tgt = logit_rows((B, K + 1, V), torch.float32, 101)
     drf = logit_rows((B, K, V), torch.float32, 102)
@@ -579,6 +578,70 @@ def test_captured_graphs():
             for c in other:
                 c()
             torch.cuda.synchronize()
+
+
+def test_captured_calls_of_many_rows():
+    """The launches of large calls (rows handed out by a counter, split rows merged,
+    accept tests in a launch of their own), captured together and replayed: each
+    replay has the eager calls' bits, also after eager calls in between, and
+    nothing is written beside the gradient."""
+    N, K, V, M = 900, 3, 32003, 40  # 173 MB of bfloat16 logits
+    z = logit_rows((N, K, V), torch.bfloat16, 201)
+    ids, val, lz = lists(N, K, V, M, 202)
+    ids[5] = -1
+    z[7, 1, 3] = torch.nan
+    p, q, di, u, us = probs(20000, 2, 24, torch.float32, 203)
+    buf = torch.full((N * K * V + 64,), 3.0, device="cuda", dtype=torch.bfloat16)
+    g = buf[31:31 + N * K * V].view(N, K, V)
+
+    def step():
+        return (tuple(binding.top_logits(z[:4], M).values())
+                + binding.distill_loss_fwd_bwd(z, ids, val, lz, scale=0.5, grad_out=g)[:2] + (g,)
+                + tuple(binding.verify_probs(p, q, di, u, us).values()))
+
+    want = _bits(step())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for rep in range(4):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(w, o) for w, o in zip(want, _bits(outs)))
+        assert (buf[:31] == 3.0).all() and (buf[-33:] == 3.0).all()
+        binding.distill_loss_fwd_bwd(z[:850], ids[:850], val[:850], lz[:850])
+        torch.cuda.synchronize()
+
+
+def test_offsets_beyond_32_bits():
+    """Rows that start 2^31 elements and more behind the first, and a gradient of more elements than that."""
+    V, far = 9001, 2 ** 31 + 12
+    buf = torch.empty(far + 4 * V, device="cuda")
+
+    def spread(t):  # the same values, the second entry of the first dimension far away
+        o = buf.as_strided(t.shape, (far, V, 1))
+        o.copy_(t)
+        return o
+
+    z = logit_rows((2, 3, V), torch.float32, 211)
+    check_top(binding.top_logits(spread(z), 30), z, 30, 1.0)
+    ids, val, lz = lists(2, 3, V, 30, 212)
+    check_distill(binding.distill_loss_fwd_bwd(spread(z), ids, val, lz), z, ids, val, lz, 1.0, "forward")
+    p, q, di, u, us = probs(2, 2, V, torch.float32, 213)
+    check_probs(binding.verify_probs(spread(p), q, di, u, us), p, q, di, u, us)
+    check_probs(binding.verify_probs(p, spread(q), di, u, us), p, q, di, u, us)
+    del buf
+    N, V, M = 14200, 151936, 16
+    row = logit_rows((1, 1, V), torch.bfloat16, 214).expand(N, 1, V)
+    ids, val, lz = (t.expand(N, *t.shape[1:]) for t in lists(1, 1, V, M, 215))
+    _, per, g = binding.distill_loss_fwd_bwd(row, ids, val, lz, grad_dtype=torch.bfloat16)
+    assert g.numel() > 2 ** 31
+    check_distill((None, per[-1:], g[-1:]), row[-1:], ids[-1:], val[-1:], lz[-1:], 1.0, "forward")
+    assert (per == per[-1]).all()
+    for n in (0, N // 2, N - 2):
+        assert torch.equal(g[n], g[-1])
 
 
 def test_given_outputs_and_workspace():
