@@ -1,8 +1,8 @@
 // probs_kernel.h — chain rejection-sampling verification from given
 // probabilities and given uniforms (paper Sec. 2.2 Eq. reject_sample, App.
-// G.1 Alg. rs_multinomial), in two launches, or three in large calls:
+// G.1 Alg. rs_multinomial), in two launches, or three in large calls of bfloat16:
 //
-//   0 probs_decide  (large calls) one wave per batch row: the accept tests.
+//   0 probs_decide  (those) one wave per batch row: the accept tests.
 //   1 probs_pass    one wave per (batch row, sub-chunk) of the emitting step,
 //                   with overlaps per (batch row, step, sub-chunk): the accept
 //                   tests from the gathered p(x_i), q(x_i), then the
@@ -13,8 +13,8 @@
 //
 // With the probabilities given, the accept tests need two gathered values a
 // step, so only the emitting step's pair (or the bonus row) is streamed.  What
-// bounds the pass is that read: B = 256, K = 3, V = 151936 float32 with overlaps 150
-// to 155 us (6.5 TB/s) and probs_finish 10; B = 1 5 us each.
+// bounds the pass is that read: B = 256, K = 3, V = 151936 float32 with overlaps 151 us
+// a call (1.0 GB, 6.7 TB/s before probs_finish's 8 to 10 us); B = 1 10 us a call.
 //
 // The accept test u q < p is exact: u and q have 24-bit significands, so their
 // product is exact in float64.  p - q and every sum of the residual are
@@ -26,8 +26,8 @@
 
 namespace sv {
 
-// Elements of a sub-chunk (one wave), read in four steps of 16 a lane.
-constexpr int kProbsSub = 4096;
+// Vectors of a load step (16 elements a lane).  A sub-chunk (one wave) has SUB
+// elements, a power of two of load steps.
 template <class E>
 constexpr int probs_step() { return 16 / E::EPV; }
 
@@ -121,7 +121,7 @@ __device__ __forceinline__ double residual(float p, float q) {
 // Units of launch 1: without overlaps (row b, sub-chunk), with them (row b,
 // step i <= K, sub-chunk), i = K being the bonus row of a row whose drafts all
 // passed.
-template <class E, bool OV>
+template <class E, bool OV, int SUB>
 __global__ __launch_bounds__(kThreads) void probs_pass_kernel(ProbsArgs a, int64_t units) {
   using raw = typename E::raw;
   constexpr int EPV = E::EPV, S = probs_step<E>();
@@ -141,11 +141,11 @@ __global__ __launch_bounds__(kThreads) void probs_pass_kernel(ProbsArgs a, int64
   const raw* prow = static_cast<const raw*>(a.p) + b * a.psb + i * a.psk;
   const raw* qrow = draft ? static_cast<const raw*>(a.q) + b * a.qsb + i * a.qsk : prow;
   const int struck = (!a.q && i < d.len) ? d.x : -1;
-  const int e0 = c * kProbsSub;
+  const int e0 = c * SUB;
   double rs = 0.0, os = 0.0;
   float lo = 0.f, hi = 0.f;
 #pragma unroll 1
-  for (int st = 0; st < kProbsSub / (S * 64 * EPV); ++st) {
+  for (int st = 0; st < SUB / (S * 64 * EPV); ++st) {
     const int es = e0 + st * S * 64 * EPV;
     if (es >= a.V) break;
     float x[S][EPV], y[S][EPV];
@@ -207,13 +207,13 @@ __device__ __forceinline__ double wg_excl_scan(double v, double* total, ProbsLds
 // The token of one sub-chunk: the first element v whose cumulative residual
 // (from `base` at the sub-chunk's start) exceeds `target`, else the last
 // element with residual (where rounding left none above), -1 if there is none.
-template <class E>
+template <class E, int SUB>
 __device__ __forceinline__ int probs_pick(const typename E::raw* prow, const typename E::raw* qrow, int struck, int V,
                                           int c, double base, double target, ProbsLds& s) {
-  constexpr int EPV = E::EPV, TILES = kProbsSub / (kThreads * EPV);
-  static_assert(TILES <= 4, "one wsum row per tile");
+  constexpr int EPV = E::EPV, TILES = SUB / (kThreads * EPV);
+  static_assert(TILES >= 1 && TILES <= 4, "one wsum row per tile");
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  const int e0 = c * kProbsSub;
+  const int e0 = c * SUB;
   float x[TILES][EPV], y[TILES][EPV];
   load_probs<E, TILES, kThreads>(prow, e0, t, V, x);
   if (qrow) {
@@ -265,15 +265,15 @@ __device__ __forceinline__ int probs_pick(const typename E::raw* prow, const typ
 
 // Sum of sub-chunk c of a row (pair) as probs_pass forms it, by one wave; for
 // the rows whose residual has no mass, whose token is drawn from p itself.
-template <class E>
+template <class E, int SUB>
 __device__ __forceinline__ double probs_sub_sum(const typename E::raw* prow, int V, int c) {
   constexpr int EPV = E::EPV, S = probs_step<E>();
   const int lane = threadIdx.x & 63;
   double rs = 0.0;
   float lo = 0.f, hi = 0.f;
 #pragma unroll 1
-  for (int st = 0; st < kProbsSub / (S * 64 * EPV); ++st) {
-    const int es = c * kProbsSub + st * S * 64 * EPV;
+  for (int st = 0; st < SUB / (S * 64 * EPV); ++st) {
+    const int es = c * SUB + st * S * 64 * EPV;
     if (es >= V) break;
     float x[S][EPV];
     load_probs<E, S, 64>(prow, es, lane, V, x);
@@ -332,7 +332,7 @@ __device__ __forceinline__ int probs_locate(const double* sums, int C, double u,
   return at;
 }
 
-template <class E>
+template <class E, int SUB>
 __global__ __launch_bounds__(kThreads) void probs_finish_kernel(ProbsArgs a) {
   using raw = typename E::raw;
   __shared__ ProbsLds s;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void probs_finish_kernel(ProbsArgs a) {
     if (c == -1 && rejected) {
       // the residual has no mass: the token is drawn from p
       for (int cc = wave; cc < a.C; cc += kWaves) {
-        const double v = probs_sub_sum<E>(prow, a.V, cc);
+        const double v = probs_sub_sum<E, SUB>(prow, a.V, cc);
         if (lane == 0) sums[cc] = v;
       }
       __syncthreads();
@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void probs_finish_kernel(ProbsArgs a) {
       struck = -1;
       c = probs_locate(sums, a.C, u, &base, &target, s);
     }
-    if (c >= 0) tok = probs_pick<E>(prow, qrow, struck, a.V, c, base, target, s);
+    if (c >= 0) tok = probs_pick<E, SUB>(prow, qrow, struck, a.V, c, base, target, s);
   }
   const bool bad = tok < 0;
   if (t == 0) a.accept_len[b] = bad ? -1 : d.n;

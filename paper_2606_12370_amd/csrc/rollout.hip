@@ -186,51 +186,67 @@ spec_status launch_distill_grad(const sv::DistillArgs& a, spec_dtype gd, hipStre
 }
 
 // ---- verification from probabilities --------------------------------------------------
+constexpr int kProbsSub = 2048;       // elements of a sub-chunk (a wave)
+constexpr int kProbsSubLarge = 4096;  // in large calls of bfloat16
+
+// (the same for every sub-chunk size: room for the smallest)
 struct ProbsLayout {
   size_t decision = 0, res = 0, ov = 0, total = 0;
-  int C = 0;
 };
 ProbsLayout probs_layout(int B, int K, int V) {
   ProbsLayout L;
-  L.C = static_cast<int>(ceil_div(V, sv::kProbsSub));
+  const size_t C = static_cast<size_t>(ceil_div(V, kProbsSub));
   size_t off = 0;
   L.decision = off; off = align_up(off + static_cast<size_t>(B) * sizeof(sv::ProbsDecision), 256);
-  L.res = off; off = align_up(off + static_cast<size_t>(B) * L.C * sizeof(double), 256);
-  L.ov = off; off = align_up(off + static_cast<size_t>(B) * K * L.C * sizeof(double), 256);
+  L.res = off; off = align_up(off + static_cast<size_t>(B) * C * sizeof(double), 256);
+  L.ov = off; off = align_up(off + static_cast<size_t>(B) * K * C * sizeof(double), 256);
   L.total = off;
   return L;
 }
 
 bool probs_sizes_ok(int B, int K, int V) {
   return B >= 1 && K >= 0 && K <= SPEC_MAX_K && V >= 1 && V <= SPEC_MAX_V &&
-         int64_t{B} * (K + 1) * ceil_div(V, 4096) < kMaxGroups * sv::kWaves && B < kMaxGroups;
+         int64_t{B} * (K + 1) * ceil_div(V, kProbsSub) < kMaxGroups * sv::kWaves && B < kMaxGroups;
 }
 
-// Units (waves of the pass) from which the accept tests take a launch of their own
-// instead of every wave taking its row's (us a call, with overlaps, K = 3; in the
-// pass / own launch: float32 V = 151936 B = 1 14.2 / 15.5, B = 256 (38912 units) 159 /
-// 161, B = 512 308.5 / 309.8; bfloat16 V = 262144 B = 64 (16384) 62.4 / 61.4, B = 256
-// (65536) 191 / 183, B = 1000 707 / 665; without overlaps B = 1000 (64000) 164 / 160).
-constexpr int64_t kProbsDecideUnits = 49152;
+// Sub-chunks of bfloat16 from which they have 4096 elements, and the accept tests a
+// launch of their own instead of every wave taking its row's.  us a call, K = 3, with
+// sub-chunks of 2048 / 4096 / 8192 elements: float32 V = 151936 without overlaps B = 1
+// 10.1 / 12.7 / 18.1, B = 64 17.4 / 19.2 / 24.9, B = 256 46.7 / 50.5 / 55.2, with them
+// B = 1 11.4 / 14.2 / 20.5, B = 256 156 / 159 / 168, B = 512 310 / 311 / 318 (1024: 10.4,
+// 156, 304, but B = 64 53 against 48); bfloat16 V = 262144 without B = 1 12.2 / 18.6 /
+// 23.7, B = 64 (8192 sub-chunks of 2048) 24.4 / 26.1 / 34, B = 256 (32768) 58.2 / 54.5 /
+// 54, B = 1000 173 / 158 / 166, with B = 16 (8192) 27.9 / 28.2 / 35.8, B = 64 (32768)
+// 65.6 / 62.3 / 62.5, B = 1000 737 / 662 / 640.  Tests in the pass / in a launch: float32
+// with overlaps B = 1 11.2 / 12.2, B = 256 151 / 156, B = 512 301 / 310; bfloat16 (4096)
+// B = 64 62.2 / 60.8, B = 256 191 / 183, B = 1000 706 / 663.
+constexpr int64_t kProbsSubUnits = 16384;
 
-template <class E>
-spec_status launch_probs(sv::ProbsArgs a, sv::ProbsDecision* decision, hipStream_t s) {
-  if (int64_t{a.B} * (a.overlap ? a.K + 1 : 1) * a.C > kProbsDecideUnits) {
-    hipLaunchKernelGGL(sv::probs_decide_kernel<E>, groups(ceil_div(a.B, sv::kWaves)), dim3(sv::kThreads), 0, s, a,
-                       decision);
-    a.decision = decision;
-  }
-  if (a.overlap) {
-    const int64_t units = int64_t{a.B} * (a.K + 1) * a.C;
-    hipLaunchKernelGGL((sv::probs_pass_kernel<E, true>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads), 0, s,
-                       a, units);
-  } else {
-    const int64_t units = int64_t{a.B} * a.C;
-    hipLaunchKernelGGL((sv::probs_pass_kernel<E, false>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads), 0, s,
-                       a, units);
-  }
-  hipLaunchKernelGGL(sv::probs_finish_kernel<E>, groups(a.B), dim3(sv::kThreads), 0, s, a);
+template <class E, int SUB>
+spec_status launch_probs_sub(sv::ProbsArgs a, hipStream_t s) {
+  a.C = static_cast<int>(ceil_div(a.V, SUB));
+  const int64_t units = int64_t{a.B} * (a.overlap ? a.K + 1 : 1) * a.C;
+  if (a.overlap)
+    hipLaunchKernelGGL((sv::probs_pass_kernel<E, true, SUB>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads),
+                       0, s, a, units);
+  else
+    hipLaunchKernelGGL((sv::probs_pass_kernel<E, false, SUB>), groups(ceil_div(units, sv::kWaves)), dim3(sv::kThreads),
+                       0, s, a, units);
+  hipLaunchKernelGGL((sv::probs_finish_kernel<E, SUB>), groups(a.B), dim3(sv::kThreads), 0, s, a);
   return launched();
+}
+
+spec_status launch_probs_f32(const sv::ProbsArgs& a, hipStream_t s) {
+  return launch_probs_sub<sv::F32, kProbsSub>(a, s);
+}
+
+spec_status launch_probs_bf16(sv::ProbsArgs a, sv::ProbsDecision* decision, hipStream_t s) {
+  if (int64_t{a.B} * (a.overlap ? a.K + 1 : 1) * ceil_div(a.V, kProbsSub) <= kProbsSubUnits)
+    return launch_probs_sub<sv::BF16, kProbsSub>(a, s);
+  hipLaunchKernelGGL(sv::probs_decide_kernel<sv::BF16>, groups(ceil_div(a.B, sv::kWaves)), dim3(sv::kThreads), 0, s, a,
+                     decision);
+  a.decision = decision;
+  return launch_probs_sub<sv::BF16, kProbsSubLarge>(a, s);
 }
 
 }  // namespace
@@ -359,7 +375,7 @@ spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int6
   a.p = target_probs; a.psb = t_stride_b; a.psk = t_stride_k;
   a.q = draft_probs; a.qsb = d_stride_b; a.qsk = d_stride_k;
   a.ids = draft_ids; a.ua = accept_uniforms; a.us = sample_uniforms; a.lens = draft_lens;
-  a.B = B; a.K = K; a.V = V; a.C = L.C;
+  a.B = B; a.K = K; a.V = V;
   a.accept_len = accept_len; a.emitted = emitted_ids;
   a.overlap = K > 0 ? overlap : nullptr;
   char* ws = static_cast<char*>(workspace);
@@ -367,7 +383,7 @@ spec_status spec_verify_probs(const void* target_probs, int64_t t_stride_b, int6
   a.ov = reinterpret_cast<double*>(ws + L.ov);
   hipStream_t s = static_cast<hipStream_t>(stream);
   sv::ProbsDecision* decision = reinterpret_cast<sv::ProbsDecision*>(ws + L.decision);
-  return dtype == SPEC_BF16 ? launch_probs<sv::BF16>(a, decision, s) : launch_probs<sv::F32>(a, decision, s);
+  return dtype == SPEC_BF16 ? launch_probs_bf16(a, decision, s) : launch_probs_f32(a, s);
 }
 
 }  // extern "C"

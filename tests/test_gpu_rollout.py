@@ -362,6 +362,16 @@ def test_probs_many_rows(B, K, V, dtype, draft):
     check_probs(binding.verify_probs(p, q, ids, u, us, want_overlap=False), p, q, ids, u, us)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("B,K,V", [(3, 2, 2047), (3, 2, 2048), (2, 2, 2049), (2, 1, 4095), (2, 1, 4096), (2, 1, 4097),
+                                   (4096, 3, 33), (4097, 3, 33), (1400, 3, 4999)])
+def test_probs_sub_chunks(B, K, V, dtype):
+    """Each side of the sub-chunks' ends, and of the number of them where bfloat16's grow."""
+    p, q, ids, u, us = probs(B, K, V, TYPES[dtype], 3 * B + V)
+    for ov in (True, False):
+        check_probs(binding.verify_probs(p, q, ids, u, us, want_overlap=ov), p, q, ids, u, us)
+
+
 @pytest.mark.parametrize("draft", [True, False])
 @pytest.mark.parametrize("dtype", DT)
 def test_probs_ragged(dtype, draft):
@@ -590,7 +600,7 @@ def test_captured_calls_of_many_rows():
     ids, val, lz = lists(N, K, V, M, 202)
     ids[5] = -1
     z[7, 1, 3] = torch.nan
-    p, q, di, u, us = probs(20000, 2, 24, torch.float32, 203)
+    p, q, di, u, us = probs(20000, 2, 24, torch.bfloat16, 203)
     buf = torch.full((N * K * V + 64,), 3.0, device="cuda", dtype=torch.bfloat16)
     g = buf[31:31 + N * K * V].view(N, K, V)
 
